@@ -9,7 +9,8 @@
  * its merging epilogue of Section 3.2.1).  Further entry points cover the
  * partial-gradient variant (Alg. 3 / Alg. 4), a per-row loss with per-row
  * upstream gradients and label smoothing, and vocabulary-sliced calls for
- * tensor / sequence parallel layouts.
+ * tensor / sequence parallel layouts, and what trains or decodes on a few logits per row: the largest
+ * logits of each row, distillation from a teacher's, a beam search's step and its states' reordering.
  *
  * Conventions common to every entry point
  *   - All tensor pointers are DEVICE pointers owned by the caller, row-major and
@@ -313,6 +314,92 @@ flce_status flce_backward_partial(const void* H, const void* W_slice, const int6
                                   int64_t ignore_index, flce_reduction reduction, flce_dtype dt, float grad_loss,
                                   void* dH_partial_out, void* dW_slice_out,
                                   void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * The largest logits of each row, the N x V logits never kept: the K largest of row i of H.W^T in descending order, equal ones
+ * (+0 and -0 among them) by ascending id, their ids, and the row's log-sum-exp over the whole vocabulary.  A NaN logit ranks
+ * above every number (and makes the row's log-sum-exp NaN).  What a teacher's lists for flce_distill_forward are made of,
+ * and what a sampler or a beam search chooses from.  Up to 64 rows W is read once, straight to the matrix instructions; more rows go
+ * through the forward's main loop, a chunk of rows at a time whose logits wait in the workspace (fp32).
+ *   K          : 1 .. 256, at most V.  V at most 2^22.
+ *   logits_out : device, N*K floats.   ids_out : device, N*K int64.   lse_out : device, N floats.
+ *   workspace  : flce_topk_workspace_bytes(N, d, V, K, dt) bytes (0: invalid shape): the logits of a chunk of rows (up to 1 GiB or 256
+ *                rows), 8 bytes per 16 to 64 of them, and the copy of H where flce_forward makes one.
+ */
+size_t flce_topk_workspace_bytes(int64_t N, int64_t d, int64_t V, int64_t K, flce_dtype dt);
+flce_status flce_topk(const void* H, const void* W, int64_t N, int64_t d, int64_t V, int64_t K, flce_dtype dt,
+                      float* logits_out, int64_t* ids_out, float* lse_out,
+                      void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Distillation from a teacher's largest logits.  Row i's list: K pairs (teacher_ids[i][k], teacher_logits[i][k]); an entry with a
+ * negative id is absent (its logit is not looked at), the others' shares are p_ik = softmax_k(teacher_logits[i][k] / T).  With
+ * T = temperature and the student's logits Z = H.W^T,
+ *   loss_i = T^2 sum_k p_ik (log p_ik - (Z_{i,id_ik} / T - lse_i)),   lse_i = log sum_v exp(Z_iv / T),
+ *   dloss_i / dZ_iv = T (exp(Z_iv / T - lse_i) - sum of the p_ik with id_ik = v).
+ * The same id may stand in a list more than once.  A row without an entry, or whose entries all have -inf, does not count: loss 0,
+ * dH row +0, nothing for dW, left out of the mean.  A row with an id >= V is treated so and latches FLCE_ERR_TARGET_RANGE
+ * (flce_last_device_status, which also gives the number of rows that count).
+ *   K             : 1 .. 256.   temperature : positive and finite, as are T^2 and 1 / T.
+ *   loss_out      : device, 1 float, the mean over the rows that count or the sum; may be NULL if loss_rows_out is not.
+ *   loss_rows_out : device, N floats; may be NULL if loss_out is not.
+ *   lse_out       : device, N floats, of the logits / T, for every row.    zt_out : device, N*K floats, the student's logits at the
+ *                   list's ids (0 where there is no share); the backward takes both back.
+ *   grad_loss     : device, 1 float, the upstream gradient of the scalar loss, or NULL;
+ *   grad_rows     : device, N floats, of the losses per row (sum semantics), or NULL: exactly one of the two.
+ * G = dloss/dZ is rounded to `dt` before the two contractions, as flce_backward's and flce_backward_rows' is.
+ * Workspaces: flce_distill_workspace_bytes(N, d, V, K, dt, for_backward) bytes, 0 for an invalid shape.  Forward: 8 bytes per 64
+ * (fp32: 32) logits of a chunk of rows (up to 256 MiB or 256 rows), the lists by tile, flce_forward's copy of H; backward:
+ * flce_backward's and 4 bytes per list entry.
+ */
+size_t flce_distill_workspace_bytes(int64_t N, int64_t d, int64_t V, int64_t K, flce_dtype dt, int for_backward);
+flce_status flce_distill_forward(const void* H, const void* W, const int64_t* teacher_ids, const float* teacher_logits,
+                                 int64_t N, int64_t d, int64_t V, int64_t K, float temperature,
+                                 flce_reduction reduction, flce_dtype dt,
+                                 float* loss_out, float* loss_rows_out, float* lse_out, float* zt_out,
+                                 void* workspace, size_t workspace_bytes, void* hip_stream);
+flce_status flce_distill_backward(const void* H, const void* W, const int64_t* teacher_ids, const float* teacher_logits,
+                                  const float* lse, const float* zt,
+                                  int64_t N, int64_t d, int64_t V, int64_t K, float temperature,
+                                  flce_reduction reduction, flce_dtype dt, const float* grad_loss, const float* grad_rows,
+                                  void* dH_out, void* dW_out,
+                                  void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * One step of a beam search.  `batch` searches of `beams` beams; beam j of search b has the hidden state H[b * beams + j], the score
+ * scores[b][j] (a sum of log-probabilities) and, if `finished` is not NULL, a flag.  Candidates of a search: for a beam that
+ * goes on every token v with scores[b][j] + (Z_v - lse), for a finished one (flag not 0) itself, with its score and pad_id.  The
+ * n_out best in descending order, equal scores by beam, then by logit, then by token; a beam whose score is NaN or +inf
+ * hands it to all its candidates, and NaN ranks above every number.  n_out may differ from beams (a first step widens one beam
+ * to several; twice the beams leave a choice to the caller).  Where there are fewer candidates than n_out, the rest have
+ * score -inf, pad_id, parent 0 and the flag set.
+ *   batch * beams rows; beams and n_out 1 .. 64; V at most 2^22.
+ *   scores_out (float), tokens_out, parents_out (int64, the beam 0 .. beams - 1 a candidate comes from), finished_out (uint8, the
+ *   parent's flag or token == eos_id; a negative eos_id matches none): device, [batch][n_out]; must not overlap scores / finished.
+ *   workspace : flce_beam_workspace_bytes(batch, beams, d, V, n_out, dt) bytes, 0 for an invalid shape.
+ */
+size_t flce_beam_workspace_bytes(int64_t batch, int64_t beams, int64_t d, int64_t V, int64_t n_out, flce_dtype dt);
+flce_status flce_beam_step(const void* H, const void* W, const float* scores, const uint8_t* finished,
+                           int64_t batch, int64_t beams, int64_t d, int64_t V, int64_t n_out,
+                           int64_t eos_id, int64_t pad_id, flce_dtype dt,
+                           float* scores_out, int64_t* tokens_out, int64_t* parents_out, uint8_t* finished_out,
+                           void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * The states of the beams after a step: row (o, b, j) of dst becomes row (o, b, parents[b][j]) of src, row_bytes of it, for o < outer
+ * (layers, keys and values), b < batch, j < beams_out.  Rows of one o lie row_stride bytes apart ([batch][beams]), the o outer_stride
+ * bytes (any strides and alignment; multiples of 16 bytes are fast).  What lies between row_bytes and row_stride is left as it
+ * was.  src and dst may be the same memory with the same strides, for beams_in == beams_out <= 16 (rows that keep their place
+ * are not touched); otherwise they must not overlap.
+ *   beams_in, beams_out : 1 .. 64.    parents : device, batch*beams_out int64.
+ *   status_out : device, one int32, or NULL: set to FLCE_ERR_TARGET_RANGE where a parent is outside [0, beams_in) (its row is left
+ *                as it was), never cleared.
+ */
+flce_status flce_beam_reorder(const void* src, void* dst, const int64_t* parents,
+                              int64_t outer, int64_t batch, int64_t beams_in, int64_t beams_out, int64_t row_bytes,
+                              int64_t src_row_stride, int64_t src_outer_stride,
+                              int64_t dst_row_stride, int64_t dst_outer_stride,
+                              int32_t* status_out, void* hip_stream);
 
 /*
  * Synchronises `hip_stream`, then reports what the last flce_forward or

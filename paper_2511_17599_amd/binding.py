@@ -22,7 +22,8 @@ FLCE_STATIC_SCRATCH_BYTES = 16 << 20
 EXPORTS = ("flce_version", "flce_tuning_reload", "flce_status_string", "flce_workspace_bytes", "flce_plan_describe", "flce_forward", "flce_backward", "flce_backward_device_grad", "flce_forward_static",
            "flce_forward_with_grads", "flce_scale", "flce_forward_rows", "flce_backward_rows", "flce_forward_partial", "flce_merge_workspace_bytes",
            "flce_merge_partials", "flce_backward_partial", "flce_last_device_status", "flce_profile_enable",
-           "flce_profile_collect", "flce_probe")
+           "flce_profile_collect", "flce_probe", "flce_topk_workspace_bytes", "flce_topk", "flce_distill_workspace_bytes",
+           "flce_distill_forward", "flce_distill_backward", "flce_beam_workspace_bytes", "flce_beam_step", "flce_beam_reorder")
 PROF_CLASSES = ("fwd_tiles", "fwd_epilogue", "bwd_prep", "recompute", "contract_dW", "contract_dH", "scale")
 
 _lib = None
@@ -99,6 +100,18 @@ def lib():
         L.flce_probe.restype = c.c_int
         L.flce_probe.argtypes = [c.c_int, c.c_void_p, c.c_void_p, c.c_void_p, c.c_int64, c.c_int64, c.c_int64, c.c_int,
                                  c.c_int, c.c_void_p, c.c_void_p]
+        p, i64, i, f, sz = c.c_void_p, c.c_int64, c.c_int, c.c_float, c.c_size_t
+        for name, restype, argtypes in (
+                ("flce_topk_workspace_bytes", sz, [i64, i64, i64, i64, i]),
+                ("flce_topk", i, [p, p, i64, i64, i64, i64, i, p, p, p, p, sz, p]),
+                ("flce_distill_workspace_bytes", sz, [i64, i64, i64, i64, i, i]),
+                ("flce_distill_forward", i, [p, p, p, p, i64, i64, i64, i64, f, i, i, p, p, p, p, p, sz, p]),
+                ("flce_distill_backward", i, [p, p, p, p, p, p, i64, i64, i64, i64, f, i, i, p, p, p, p, p, sz, p]),
+                ("flce_beam_workspace_bytes", sz, [i64, i64, i64, i64, i64, i]),
+                ("flce_beam_step", i, [p, p, p, p, i64, i64, i64, i64, i64, i64, i64, i, p, p, p, p, p, sz, p]),
+                ("flce_beam_reorder", i, [p, p, p, i64, i64, i64, i64, i64, i64, i64, i64, i64, p, p])):
+            fn = getattr(L, name)
+            fn.restype, fn.argtypes = restype, argtypes
         _lib = L
     return _lib
 
@@ -219,6 +232,51 @@ def flce_backward_partial(H, W_slice, targets, lse, N, d, V_slice, v_begin, V_to
     return lib().flce_backward_partial(_ptr(H), _ptr(W_slice), _ptr(targets), _ptr(lse), N, d, V_slice, v_begin,
                                        V_total, ignore_index, reduction, dt, float(grad_loss), _ptr(dH_partial_out),
                                        _ptr(dW_slice_out), _ptr(workspace), workspace_bytes, _stream(hip_stream))
+
+
+def flce_topk_workspace_bytes(N, d, V, K, dt):
+    return int(lib().flce_topk_workspace_bytes(N, d, V, K, dt))
+
+
+def flce_topk(H, W, N, d, V, K, dt, logits_out, ids_out, lse_out, workspace, workspace_bytes, hip_stream=None):
+    return lib().flce_topk(_ptr(H), _ptr(W), N, d, V, K, dt, _ptr(logits_out), _ptr(ids_out), _ptr(lse_out), _ptr(workspace),
+                           workspace_bytes, _stream(hip_stream))
+
+
+def flce_distill_workspace_bytes(N, d, V, K, dt, for_backward):
+    return int(lib().flce_distill_workspace_bytes(N, d, V, K, dt, int(bool(for_backward))))
+
+
+def flce_distill_forward(H, W, teacher_ids, teacher_logits, N, d, V, K, temperature, reduction, dt, loss_out, loss_rows_out,
+                         lse_out, zt_out, workspace, workspace_bytes, hip_stream=None):
+    return lib().flce_distill_forward(_ptr(H), _ptr(W), _ptr(teacher_ids), _ptr(teacher_logits), N, d, V, K,
+                                      float(temperature), reduction, dt, _ptr(loss_out), _ptr(loss_rows_out), _ptr(lse_out),
+                                      _ptr(zt_out), _ptr(workspace), workspace_bytes, _stream(hip_stream))
+
+
+def flce_distill_backward(H, W, teacher_ids, teacher_logits, lse, zt, N, d, V, K, temperature, reduction, dt, grad_loss,
+                          grad_rows, dH_out, dW_out, workspace, workspace_bytes, hip_stream=None):
+    return lib().flce_distill_backward(_ptr(H), _ptr(W), _ptr(teacher_ids), _ptr(teacher_logits), _ptr(lse), _ptr(zt), N, d, V,
+                                       K, float(temperature), reduction, dt, _ptr(grad_loss), _ptr(grad_rows), _ptr(dH_out),
+                                       _ptr(dW_out), _ptr(workspace), workspace_bytes, _stream(hip_stream))
+
+
+def flce_beam_workspace_bytes(batch, beams, d, V, n_out, dt):
+    return int(lib().flce_beam_workspace_bytes(batch, beams, d, V, n_out, dt))
+
+
+def flce_beam_step(H, W, scores, finished, batch, beams, d, V, n_out, eos_id, pad_id, dt, scores_out, tokens_out, parents_out,
+                   finished_out, workspace, workspace_bytes, hip_stream=None):
+    return lib().flce_beam_step(_ptr(H), _ptr(W), _ptr(scores), _ptr(finished), batch, beams, d, V, n_out, eos_id, pad_id, dt,
+                                _ptr(scores_out), _ptr(tokens_out), _ptr(parents_out), _ptr(finished_out), _ptr(workspace),
+                                workspace_bytes, _stream(hip_stream))
+
+
+def flce_beam_reorder(src, dst, parents, outer, batch, beams_in, beams_out, row_bytes, src_row_stride, src_outer_stride,
+                      dst_row_stride, dst_outer_stride, status_out=None, hip_stream=None):
+    return lib().flce_beam_reorder(_ptr(src), _ptr(dst), _ptr(parents), outer, batch, beams_in, beams_out, row_bytes,
+                                   src_row_stride, src_outer_stride, dst_row_stride, dst_outer_stride, _ptr(status_out),
+                                   _stream(hip_stream))
 
 
 def flce_last_device_status(workspace, hip_stream=None):

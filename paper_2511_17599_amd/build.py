@@ -12,9 +12,12 @@ from __future__ import annotations
 import os
 import shutil
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 SRC = os.path.join(PKG, "csrc", "flce.hip")
+SOURCES = [SRC] + [os.path.join(PKG, "csrc", f) for f in ("topk.hip", "distill.hip")]
 LIB = os.path.join(PKG, "libflce.so")
 
 HIPCC_FLAGS = [
@@ -29,14 +32,22 @@ def hipcc_path():
     return shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
 
 
-def build_library(verbose=False):
-    """Compiles csrc/flce.hip into libflce.so next to this file; returns its path."""
-    cmd = [hipcc_path(), *HIPCC_FLAGS, SRC, "-o", LIB + ".tmp"]
+def _run(cmd, verbose):
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError("hipcc failed:\n" + res.stdout + res.stderr)
+
+
+def build_library(verbose=False):
+    """Compiles the sources under csrc/ side by side and links them into libflce.so next to this file; returns its path."""
+    flags = [f for f in HIPCC_FLAGS if f != "-shared"]
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, os.path.basename(s) + ".o") for s in SOURCES]
+        with ThreadPoolExecutor(len(SOURCES)) as pool:
+            list(pool.map(lambda so: _run([hipcc_path(), *flags, "-c", so[0], "-o", so[1]], verbose), zip(SOURCES, objects)))
+        _run([hipcc_path(), "--offload-arch=gfx950", "-fPIC", "-shared", *objects, "-o", LIB + ".tmp"], verbose)
     os.replace(LIB + ".tmp", LIB)
     return LIB
 

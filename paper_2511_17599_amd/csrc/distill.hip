@@ -1,0 +1,201 @@
+// C-ABI entry points of the distillation from a teacher's largest logits (see include/flce.h).  Host code: checks, workspaces,
+// launches; the backward is the cross-entropy's with another recompute step.
+#include <algorithm>
+#include <cmath>
+
+#include "distill.h"
+
+namespace flce {
+
+template <typename T, typename L>
+hipError_t distill_recompute(const RecomputeArgs<T>& a, int grid, const DistillLists& lists, const int* rowmap, bool per_row,
+                             hipStream_t st) {
+  static OncePerDevice once;
+  const hipError_t e = once([] {
+    const hipError_t e = allow_big_lds(recompute_kernel<T, L, L::TUNED, false, true>, L::LDS);
+    return e != hipSuccess ? e : allow_big_lds(recompute_kernel<T, L, L::TUNED, true, true>, L::LDS);
+  });
+  if (e != hipSuccess) return e;
+  RecomputeTempArgs<T> x;
+  static_cast<RecomputeArgs<T>&>(x) = a;
+  x.z_scale = lists.z_scale;
+  const unsigned blocks = (unsigned)ceil_div((int64_t)a.n_nt * L::TILE * lists.K, 256);
+  if (per_row) {
+    recompute_kernel<T, L, L::TUNED, true, true><<<grid, L::THREADS, L::LDS, st>>>(x);
+    distill_scatter_kernel<T, L, true><<<blocks, 256, 0, st>>>(a, lists, rowmap);
+  } else {
+    recompute_kernel<T, L, L::TUNED, false, true><<<grid, L::THREADS, L::LDS, st>>>(x);
+    distill_scatter_kernel<T, L, false><<<blocks, 256, 0, st>>>(a, lists, rowmap);
+  }
+  return hipSuccess;
+}
+#define FLCE_DISTILL(T, ...) \
+  template hipError_t distill_recompute<T, __VA_ARGS__>(const RecomputeArgs<T>&, int, const DistillLists&, const int*, bool, hipStream_t);
+FLCE_DISTILL(bf16_t, SmallLoop<true>)
+FLCE_DISTILL(bf16_t, SmallLoop<false>)
+FLCE_DISTILL(bf16_t, FastLoop<true>)
+FLCE_DISTILL(bf16_t, FastLoop<false>)
+FLCE_DISTILL(bf16_t, GenericLoop)
+FLCE_DISTILL(float, F32Loop<64>)
+FLCE_DISTILL(float, F32Loop<128>)
+#undef FLCE_DISTILL
+
+namespace {
+
+// The groups' pairs of a chunk of rows wait in memory for their sum.
+constexpr int64_t DISTILL_STATS_BYTES = (int64_t)256 << 20;
+
+struct DistillPlan {
+  Plan p;
+  int tile, group, n_groups, n_blk;
+  int64_t ld_stats, rows;
+  int64_t off_blk_loss, off_blk_cnt, off_blk_oor, off_stats, off_begin, off_entries, off_HT, fwd_bytes;
+  int64_t off_share, off_target, off_grad, off_grad_rows, bwd_bytes;
+};
+
+bool make_distill_plan(int parts, int64_t N, int64_t d, int64_t V, int64_t K, flce_dtype dt, DistillPlan& x) {
+  if (!make_plan(parts, N, d, V, dt, x.p) || K < 1 || K > DISTILL_MAX) return false;
+  const Plan& p = x.p;
+  if (parts & PLAN_FORWARD) {
+    x.tile = p.esize == 2 && !p.fast ? TILE : p.fwd_tile;
+    x.group = p.fast ? 64 : 32;
+    x.n_groups = (int)ceil_div(V, x.group);
+    x.ld_stats = align_up(V, TILE) / x.group;
+    const int64_t most = std::max<int64_t>(TILE, DISTILL_STATS_BYTES / (x.ld_stats * 8) / TILE * TILE);
+    x.rows = align_up(ceil_div(p.npad, ceil_div(p.npad, most)), TILE);
+    x.n_blk = 0;
+    for (int64_t r = 0; r < N; r += x.rows) x.n_blk += (int)ceil_div(std::min(x.rows, N - r), DISTILL_ROWS);
+    const int64_t n_rt = ceil_div(N, x.tile), n_vt = ceil_div(V, x.tile);
+    int64_t o = ALIGN;
+    x.off_blk_loss = o; o = align_up(o + (int64_t)x.n_blk * 4, ALIGN);
+    x.off_blk_cnt = o;  o = align_up(o + (int64_t)x.n_blk * 4, ALIGN);
+    x.off_blk_oor = o;  o = align_up(o + (int64_t)x.n_blk * 4, ALIGN);
+    x.off_stats = o;    o = align_up(o + x.rows * x.ld_stats * 8, ALIGN);
+    x.off_begin = o;    o = align_up(o + n_rt * (n_vt + 1) * 4, ALIGN);
+    x.off_entries = o;  o = align_up(o + n_rt * x.tile * K * 4, ALIGN);
+    x.off_HT = o;       if (p.fwd_copy) o = align_up(o + packed_block_offset(p.n_rb, (int)d), ALIGN);
+    x.fwd_bytes = o;
+  }
+  if (parts & PLAN_BACKWARD) {
+    int64_t o = align_up(p.bwd_bytes, ALIGN);
+    x.off_share = o;     o = align_up(o + N * K * 4, ALIGN);
+    x.off_target = o;    o = align_up(o + N * 8, ALIGN);
+    x.off_grad = o;      o += ALIGN;
+    x.off_grad_rows = o; o = align_up(o + N * 4, ALIGN);
+    x.bwd_bytes = o;
+  }
+  return true;
+}
+
+bool temperature_ok(float T) { return T > 0.f && std::isfinite(T) && std::isfinite(LOG2E / T) && std::isfinite(T * T) && T * T > 0.f; }
+bool bad_workspace(const void* ws, size_t bytes, int64_t need) {
+  return !ws || (reinterpret_cast<uintptr_t>(ws) & 255u) || bytes < (size_t)need;
+}
+
+}  // namespace
+}  // namespace flce
+
+extern "C" {
+
+size_t flce_distill_workspace_bytes(int64_t N, int64_t d, int64_t V, int64_t K, flce_dtype dt, int for_backward) {
+  flce::DistillPlan x;
+  if (!flce::make_distill_plan(for_backward ? flce::PLAN_BACKWARD : flce::PLAN_FORWARD, N, d, V, K, dt, x)) return 0;
+  return (size_t)(for_backward ? x.bwd_bytes : x.fwd_bytes);
+}
+
+flce_status flce_distill_forward(const void* H, const void* W, const int64_t* teacher_ids, const float* teacher_logits, int64_t N, int64_t d,
+                                 int64_t V, int64_t K, float temperature, flce_reduction reduction, flce_dtype dt, float* loss_out,
+                                 float* loss_rows_out, float* lse_out, float* zt_out, void* workspace, size_t workspace_bytes,
+                                 void* hip_stream) {
+  using namespace flce;
+  if (!H || !W || !teacher_ids || !teacher_logits || (!loss_out && !loss_rows_out) || !lse_out || !zt_out) return FLCE_ERR_BAD_ARG;
+  if (reduction != FLCE_REDUCE_MEAN && reduction != FLCE_REDUCE_SUM) return FLCE_ERR_BAD_ARG;
+  if (dt != FLCE_DTYPE_BF16 && dt != FLCE_DTYPE_F32) return FLCE_ERR_BAD_ARG;
+  if (!temperature_ok(temperature)) return FLCE_ERR_BAD_ARG;
+  DistillPlan x;
+  if (!make_distill_plan(PLAN_FORWARD, N, d, V, K, dt, x)) return FLCE_ERR_BAD_SHAPE;
+  if (!aligned16(H) || !aligned16(W)) return FLCE_ERR_BAD_ARG;
+  if (bad_workspace(workspace, workspace_bytes, x.fwd_bytes)) return FLCE_ERR_WORKSPACE;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  char* ws = static_cast<char*>(workspace);
+  const Plan& p = x.p;
+  Header* hdr = reinterpret_cast<Header*>(ws);
+  float2* stats = reinterpret_cast<float2*>(ws + x.off_stats);
+  int* begin = reinterpret_cast<int*>(ws + x.off_begin);
+  uint32_t* entries = reinterpret_cast<uint32_t*>(ws + x.off_entries);
+  void* HT = p.fwd_copy ? ws + x.off_HT : nullptr;
+  if (HT) pack_rows(p, H, HT, st);
+  return with_forward_loop(p, [&](auto tag) -> flce_status {
+    using T = typename decltype(tag)::T;
+    using L = typename decltype(tag)::L;
+    if (logit_tiles_allowance<T, L, false>() != hipSuccess) return FLCE_ERR_HIP;
+    const int n_vt = (int)ceil_div(V, L::TILE);
+    {
+      ProfScope ps(FLCE_PROF_FWD_EPILOGUE, st);
+      distill_lists_kernel<L::TILE><<<(unsigned)ceil_div(N, L::TILE), 1024, 0, st>>>(teacher_ids, teacher_logits, (int)N, (int)V, (int)K, n_vt,
+                                                                                     begin, entries, zt_out, hdr);
+    }
+    int blk0 = 0;
+    for (int64_t row0 = 0; row0 < N; row0 += x.rows) {
+      const int64_t rows = std::min<int64_t>(x.rows, N - row0);
+      LogitArgs<T> a{};
+      a.H = static_cast<const T*>(H); a.HT = static_cast<const T*>(HT); a.W = static_cast<const T*>(W);
+      a.N = (int)N; a.d = (int)d; a.V = (int)V;
+      a.nt0 = (int)(row0 / L::TILE); a.n_nt = (int)ceil_div(rows, L::TILE); a.n_vt = n_vt;
+      a.z_scale = LOG2E / temperature;
+      a.stats = stats; a.ld_stats = x.ld_stats;
+      a.list_begin = begin; a.entries = entries; a.K = (int)K; a.zt = zt_out;
+      {
+        ProfScope ps(FLCE_PROF_FWD_TILES, st);
+        launch_logit_tiles<T, L, false>(a, st);
+      }
+      ProfScope ps(FLCE_PROF_FWD_EPILOGUE, st);
+      const int n_blk = (int)ceil_div(rows, DISTILL_ROWS);
+      // a call for rows alone has no scalar loss to hand out: the sum goes to a spare word of the header block
+      float* scalar = loss_out ? loss_out : reinterpret_cast<float*>(ws + 64);
+      distill_rows_kernel<<<n_blk, 64 * DISTILL_ROWS, 0, st>>>(DistillRowArgs{
+          teacher_ids, teacher_logits, zt_out, (int)row0, (int)rows, (int)V, (int)K, x.n_groups, stats, x.ld_stats, temperature,
+          1.f / temperature, LOG2E / temperature, lse_out, loss_rows_out,
+          LossOut{reinterpret_cast<float*>(ws + x.off_blk_loss), reinterpret_cast<int*>(ws + x.off_blk_cnt),
+                  reinterpret_cast<int*>(ws + x.off_blk_oor), hdr, scalar, reduction == FLCE_REDUCE_MEAN, nullptr, nullptr},
+          blk0, x.n_blk});
+      blk0 += n_blk;
+    }
+    return hipGetLastError() == hipSuccess ? FLCE_OK : FLCE_ERR_HIP;
+  });
+}
+
+flce_status flce_distill_backward(const void* H, const void* W, const int64_t* teacher_ids, const float* teacher_logits, const float* lse,
+                                  const float* zt, int64_t N, int64_t d, int64_t V, int64_t K, float temperature, flce_reduction reduction,
+                                  flce_dtype dt, const float* grad_loss, const float* grad_rows, void* dH_out, void* dW_out,
+                                  void* workspace, size_t workspace_bytes, void* hip_stream) {
+  using namespace flce;
+  if (!H || !W || !teacher_ids || !teacher_logits || !lse || !zt || !dH_out || !dW_out) return FLCE_ERR_BAD_ARG;
+  if (!grad_loss == !grad_rows) return FLCE_ERR_BAD_ARG;
+  if (reduction != FLCE_REDUCE_MEAN && reduction != FLCE_REDUCE_SUM) return FLCE_ERR_BAD_ARG;
+  if (dt != FLCE_DTYPE_BF16 && dt != FLCE_DTYPE_F32) return FLCE_ERR_BAD_ARG;
+  if (!temperature_ok(temperature)) return FLCE_ERR_BAD_ARG;
+  DistillPlan x;
+  if (!make_distill_plan(PLAN_BACKWARD, N, d, V, K, dt, x)) return FLCE_ERR_BAD_SHAPE;
+  if (!aligned16(H) || !aligned16(W) || !aligned16(dH_out) || !aligned16(dW_out)) return FLCE_ERR_BAD_ARG;
+  if (bad_workspace(workspace, workspace_bytes, x.bwd_bytes)) return FLCE_ERR_WORKSPACE;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  char* ws = static_cast<char*>(workspace);
+  float* share = reinterpret_cast<float*>(ws + x.off_share);
+  int64_t* target = reinterpret_cast<int64_t*>(ws + x.off_target);
+  float* grad = reinterpret_cast<float*>(ws + x.off_grad);
+  float* grad_n = reinterpret_cast<float*>(ws + x.off_grad_rows);
+  {
+    ProfScope ps(FLCE_PROF_BWD_PREP, st);
+    distill_prep_kernel<<<(unsigned)ceil_div(N, DISTILL_ROWS), 64 * DISTILL_ROWS, 0, st>>>(
+        DistillPrepArgs{teacher_ids, teacher_logits, (int)N, (int)V, (int)K, 1.f / temperature, temperature, share, target, grad_loss,
+                        grad_rows, grad, grad_n});
+  }
+  const DistillLists lists{teacher_ids, share, zt, lse, (int)K, LOG2E / temperature};
+  // one vocabulary position more than W has: the targets of rows that count lie there
+  return backward_impl(H, W, target, lse, N, d, V, -1, grad_rows ? FLCE_REDUCE_SUM : reduction, dt,
+                       grad_rows ? GradLoss{1.f, nullptr} : GradLoss{0.f, grad}, dH_out, dW_out, workspace, workspace_bytes, hip_stream,
+                       Slice{V + 1, 0}, PerRow{nullptr, grad_rows ? grad_n : nullptr, 0.f}, &lists);
+}
+
+}  // extern "C"

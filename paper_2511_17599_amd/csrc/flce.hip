@@ -1,10 +1,6 @@
 // C-ABI entry points of libflce (see include/flce.h): argument checks, the launch
 // plan (windows, chunks, workspace layout) and the launch sequences.  Host code
 // only; every step of the path runs in the kernels of kernels.h.
-#include "../../include/flce.h"
-
-#include <hip/hip_runtime.h>
-
 #include <algorithm>
 #include <cstdio>
 #include <cstdlib>
@@ -12,6 +8,7 @@
 #include <vector>
 
 #include "kernels.h"
+#include "plan.h"
 #include "probe.h"
 
 // Workspace of flce_forward_static, the forward for callers that cannot allocate: a file-scope device array.
@@ -22,19 +19,10 @@ static __device__ __align__(256) unsigned char scratch[FLCE_STATIC_SCRATCH_BYTES
 namespace flce {
 namespace {
 
-constexpr int64_t ALIGN = 256;
-constexpr int NUM_CU = 256;   // MI355X; the plan must not depend on a device query
 // Most K slices of a contraction launch.  One output tile (256 rows, d <= 256) over a long vocabulary is where many help:
 // 256 rows, d = 128, V = 82194 has 321 K tiles; with 8 slices (8 busy CUs)
 // the whole step took 318 us, with 64 it takes 134 (200 x 1024 x 50257: 317 and 210).
 constexpr int MAX_SPLIT = 64;
-// Most bytes that a plan spends on the forward's copy of H at a ragged hidden size, and on the fp32 tiles of the K slices of
-// one contraction launch (60000 random shapes up to 140000 x 8192 x 262144: five would take more, 617 MB at most).
-constexpr int64_t BYTES_CAP = (int64_t)512 << 20;
-
-int64_t align_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
 int env_int(const char* name, int dflt, int lo, int hi) {
   const char* s = std::getenv(name);
   if (!s || !*s) return dflt;
@@ -72,29 +60,6 @@ Tuning tuning() {
   if (!g_tuning_loaded) { g_tuning = read_tuning_from_env(); g_tuning_loaded = true; }
   return g_tuning;
 }
-
-struct Plan {
-  int64_t N, d, V;
-  int esize;
-  int n_rb, n_vt;          // 256-row tiles of tokens / vocabulary
-  int tile, fwd_tile;      // output tile edge of the main loop, backward and forward (bf16: 256 or 128, fp32: 128 or 64)
-  int64_t npad;
-  // forward
-  int n_win;
-  int64_t off_part, off_blk_loss, off_blk_cnt, off_blk_oor, off_wpart, off_wsum, off_zbar, off_fHT, fwd_bytes;
-  // backward
-  int n_vch, n_nch;        // chunks along vocabulary / tokens
-  int vc_tiles, nc_tiles;  // largest chunk, in tiles
-  int64_t ld_v, ld_n;      // elements per row of the buffers whose rows run over a vocabulary / row chunk: the
-                           // chunk's extent plus 64, so that rows never lie a power of two apart
-  bool fast;               // tuned bf16 loop: W, Hc and G read in place by the contractions
-  bool ragged;             // its form for hidden sizes that are no multiple of a K step's 32 elements
-  bool hkr;                // forward / recompute read a pre-tiled copy of H (tuned loop, unless the caller rules the copy out)
-  bool fwd_copy;           // the forward makes that copy (long enough for it to pay)
-  int split_dh, split_dw;  // K slices of the dH / dW contraction launches (1 = unsplit)
-  bool pair;               // dW and dH of the only chunk go out as one launch
-  int64_t off_Hc, off_rowmap, off_tgt, off_lsec, off_gamc, off_HT, off_WT, off_G, off_GT, off_dHacc, off_dWacc, off_partial, off_partial_dh, bwd_bytes;
-};
 
 // A contraction launch of more than one round of workgroups whose last round would be mostly empty: the output-row
 // tiles of that last round ("tail") are launched on their own with their K extent cut into `slices` slices (summed
@@ -397,15 +362,18 @@ void plan_backward(const Tuning& tn, Plan& p) {
   p.bwd_bytes = o;
 }
 
-enum : int { PLAN_FORWARD = 1, PLAN_BACKWARD = 2, PLAN_BOTH = 3 };   // 0: the shape's check only
+}  // namespace
+
 // allow_h_copy: the caller has a workspace for the pre-tiled copy of H.
-bool make_plan(int parts, int64_t N, int64_t d, int64_t V, flce_dtype dt, Plan& p, bool allow_h_copy = true, bool wide = true) {
+bool make_plan(int parts, int64_t N, int64_t d, int64_t V, flce_dtype dt, Plan& p, bool allow_h_copy, bool wide) {
   const Tuning tn = tuning();
   if (!plan_base(N, d, V, dt, tn, allow_h_copy, p)) return false;
   if (parts & PLAN_FORWARD) plan_forward(tn, wide, p);
   if (parts & PLAN_BACKWARD) plan_backward(tn, p);
   return true;
 }
+
+namespace {
 
 // Optional per-launch event timing (flce_profile_*).
 struct ProfRec { int cls; hipEvent_t a, b; };
@@ -423,30 +391,23 @@ struct Prof {
 };
 Prof g_prof;
 
-struct ProfScope {
-  hipStream_t st;
-  hipEvent_t b = nullptr;
-  ProfScope(int cls, hipStream_t s) : st(s) {
-    if (!g_prof.on) return;
-    std::lock_guard<std::mutex> lk(g_prof.mu);
-    hipEvent_t a = g_prof.get();
-    b = g_prof.get();
-    if (!a || !b) { b = nullptr; return; }
-    (void)hipEventRecord(a, st);
-    g_prof.recs.push_back(ProfRec{cls, a, b});
-  }
-  ~ProfScope() { if (b) (void)hipEventRecord(b, st); }
-};
+}  // namespace
 
-template <typename K>
-hipError_t allow_big_lds(K kernel, int bytes) {
-  return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+ProfScope::ProfScope(int cls, hipStream_t s) : st(s) {
+  if (!g_prof.on) return;
+  std::lock_guard<std::mutex> lk(g_prof.mu);
+  hipEvent_t a = g_prof.get();
+  b = g_prof.get();
+  if (!a || !b) { b = nullptr; return; }
+  (void)hipEventRecord(a, st);
+  g_prof.recs.push_back(ProfRec{cls, a, b});
 }
+ProfScope::~ProfScope() { if (b) (void)hipEventRecord(b, st); }
+
+namespace {
 
 // The kernels of one (storage type, main loop) pair need the large dynamic LDS allowance; it is a property of
 // the loaded code object on a device, so it is set once per device and pair, not per call.
-constexpr int MAX_DEVICES = 64;
-
 template <typename T, typename L>
 hipError_t set_lds_allowances() {
   hipError_t e;
@@ -487,15 +448,6 @@ hipError_t prepare_kernels() {
   return hipSuccess;
 }
 
-// W holds the p.V vocabulary rows [slice.v_begin, slice.v_begin + p.V) of slice.V_total.  With m_out set the
-// call stops after the window merge and hands out the slice's (m, a, z_target) per row.
-struct Slice { int64_t V_total, v_begin; };
-// Per-row variant: the forward writes one loss per row (label-smoothed by eps), the backward takes one
-// upstream gradient per row (device arrays of N floats).
-struct PerRow { float* loss_rows_out; const float* grad_rows; float eps; };
-// Device words of the caller that receive the range flag and the number of counted rows (either may be null).
-struct StatusOut { int32_t* status; int64_t* n_valid; };
-
 // The window merge.  While a row's parts fit one batch of loads, one thread merges them; otherwise 16 threads do where
 // the block sums of 64-row blocks fit the arrays (they are padded to 64 entries, and many windows mean few row blocks),
 // and 4 threads in 256-row blocks elsewhere.  `launch` gets the kernel's shape: rows, threads per row, loads in flight.
@@ -523,6 +475,16 @@ int launch_merge(const float* pm, const float* pa, const float* pz, int n_parts,
   });
 }
 
+}  // namespace
+
+void pack_rows(const Plan& p, const void* H, void* HT, hipStream_t st) {
+  ProfScope ps(FLCE_PROF_FWD_EPILOGUE, st);
+  pack_rows_kernel<<<dim3((unsigned)(p.npad / 64), (unsigned)ceil_div(p.d, 128)), 256, 0, st>>>(
+      static_cast<const char*>(H), (int)p.N, (int)p.d, static_cast<char*>(HT));
+}
+
+namespace {
+
 template <typename T, typename U, typename L>
 flce_status forward_t(const Plan& p, const void* H, const void* W, const int64_t* y, int64_t ignore_index,
                       int mean, float* loss_out, float* lse_out, char* ws, hipStream_t st, Slice slice,
@@ -548,9 +510,7 @@ flce_status forward_t(const Plan& p, const void* H, const void* W, const int64_t
     if constexpr (L::TUNED) {
       HT = reinterpret_cast<T*>(ws + p.off_fHT);
       // the pre-tiled copy of H, zero padded to whole row blocks: the forward's second operand
-      ProfScope ps(FLCE_PROF_FWD_EPILOGUE, st);
-      pack_rows_kernel<<<dim3((unsigned)(p.npad / 64), (unsigned)ceil_div(p.d, 128)), 256, 0, st>>>(
-          static_cast<const char*>(H), (int)p.N, (int)p.d, reinterpret_cast<char*>(HT));
+      pack_rows(p, H, HT, st);
     }
   }
   {
@@ -605,7 +565,8 @@ flce_status forward_t(const Plan& p, const void* H, const void* W, const int64_t
 template <typename T, typename U, typename L>
 flce_status backward_t(const Plan& p, const void* H, const void* W, const int64_t* y, const float* lse,
                        int64_t ignore_index, int mean, GradLoss grad_loss, void* dH, void* dW, char* ws,
-                       hipStream_t st, Slice slice, PerRow rows = PerRow{nullptr, nullptr, 0.f}) {
+                       hipStream_t st, Slice slice, PerRow rows = PerRow{nullptr, nullptr, 0.f},
+                       const DistillLists* lists = nullptr) {
   if (prepare_kernels<T, L>() != hipSuccess) return FLCE_ERR_HIP;
   if (L::TUNED && !p.hkr) return FLCE_ERR_UNSUPPORTED;   // (no caller plans a backward without the copies of H)
   const int N = (int)p.N, d = (int)p.d, V = (int)p.V;
@@ -804,7 +765,9 @@ flce_status backward_t(const Plan& p, const void* H, const void* W, const int64_
         // at most as many workgroups as fit the chip: each walks its share of the chunk's tiles
         int grid = rc.n_nt * rc.n_vt;
         if constexpr (L::TUNED) grid = std::min(grid, NUM_CU * L::PER_CU);
-        if constexpr (L::TUNED) {     // the tuned loop's backward always has the pre-tiled copies
+        if (lists) {
+          if (distill_recompute<T, L>(rc, grid, *lists, rowmap, rows.grad_rows != nullptr, st) != hipSuccess) return FLCE_ERR_HIP;
+        } else if constexpr (L::TUNED) {     // the tuned loop's backward always has the pre-tiled copies
           if (rows.grad_rows) recompute_kernel<T, L, true, true><<<grid, L::THREADS, L::LDS, st>>>(rc);
           else recompute_kernel<T, L, true><<<grid, L::THREADS, L::LDS, st>>>(rc);
         } else {
@@ -829,8 +792,6 @@ flce_status backward_t(const Plan& p, const void* H, const void* W, const int64_
   }
   return hipGetLastError() == hipSuccess ? FLCE_OK : FLCE_ERR_HIP;
 }
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 constexpr size_t STATIC_SCRATCH_BYTES = FLCE_STATIC_SCRATCH_BYTES;
 
@@ -858,6 +819,42 @@ hipError_t static_scratch(void** out) {
 
 }  // namespace
 }  // namespace flce
+
+flce_status flce::backward_impl(const void* H, const void* W, const int64_t* targets, const float* lse, int64_t N,
+                                 int64_t d, int64_t V, int64_t ignore_index, flce_reduction reduction, flce_dtype dt,
+                                 flce::GradLoss grad_loss, void* dH_out, void* dW_out, void* workspace,
+                                 size_t workspace_bytes, void* hip_stream, flce::Slice slice,
+                                 flce::PerRow rows, const flce::DistillLists* lists) {
+  if (!H || !W || !targets || !lse || !dH_out || !dW_out) return FLCE_ERR_BAD_ARG;
+  if (!(rows.eps >= 0.f && rows.eps < 1.f)) return FLCE_ERR_BAD_ARG;
+  if (reduction != FLCE_REDUCE_MEAN && reduction != FLCE_REDUCE_SUM) return FLCE_ERR_BAD_ARG;
+  if (dt != FLCE_DTYPE_BF16 && dt != FLCE_DTYPE_F32) return FLCE_ERR_BAD_ARG;
+  flce::Plan p;
+  if (!flce::make_plan(flce::PLAN_BACKWARD, N, d, V, dt, p)) return FLCE_ERR_BAD_SHAPE;
+  if (slice.v_begin < 0 || slice.v_begin + V > slice.V_total) return FLCE_ERR_BAD_SHAPE;
+  if (!flce::aligned16(H) || !flce::aligned16(W) || !flce::aligned16(dH_out) || !flce::aligned16(dW_out))
+    return FLCE_ERR_BAD_ARG;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < (size_t)p.bwd_bytes)
+    return FLCE_ERR_WORKSPACE;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  const int mean = reduction == FLCE_REDUCE_MEAN;
+  char* ws = static_cast<char*>(workspace);
+  if (dt == FLCE_DTYPE_BF16) {
+    if (p.ragged && p.tile == 128)
+      return flce::backward_t<flce::bf16_t, uint16_t, flce::SmallLoop<true>>(p, H, W, targets, lse, ignore_index, mean, grad_loss, dH_out, dW_out, ws, st, slice, rows, lists);
+    if (p.ragged)
+      return flce::backward_t<flce::bf16_t, uint16_t, flce::FastLoop<true>>(p, H, W, targets, lse, ignore_index, mean, grad_loss, dH_out, dW_out, ws, st, slice, rows, lists);
+    if (p.fast && p.tile == 128)
+      return flce::backward_t<flce::bf16_t, uint16_t, flce::SmallLoop<false>>(p, H, W, targets, lse, ignore_index, mean, grad_loss, dH_out, dW_out, ws, st, slice, rows, lists);
+    if (p.fast)
+      return flce::backward_t<flce::bf16_t, uint16_t, flce::FastLoop<false>>(p, H, W, targets, lse, ignore_index, mean, grad_loss, dH_out, dW_out, ws, st, slice, rows, lists);
+    return flce::backward_t<flce::bf16_t, uint16_t, flce::GenericLoop>(
+        p, H, W, targets, lse, ignore_index, mean, grad_loss, dH_out, dW_out, ws, st, slice, rows, lists);
+  }
+  if (p.tile == 64)
+    return flce::backward_t<float, uint32_t, flce::F32Loop<64>>(p, H, W, targets, lse, ignore_index, mean, grad_loss, dH_out, dW_out, ws, st, slice, rows, lists);
+  return flce::backward_t<float, uint32_t, flce::F32Loop<128>>(p, H, W, targets, lse, ignore_index, mean, grad_loss, dH_out, dW_out, ws, st, slice, rows, lists);
+}
 
 extern "C" {
 
@@ -946,42 +943,6 @@ static flce_status forward_impl(const void* H, const void* W, const int64_t* tar
   return flce::forward_t<float, uint32_t, flce::F32Loop<128>>(p, H, W, targets, ignore_index, mean, loss_out, lse_out, ws, st, slice, m_out, a_out, zt_out, rows, so);
 }
 
-static flce_status backward_impl(const void* H, const void* W, const int64_t* targets, const float* lse, int64_t N,
-                                 int64_t d, int64_t V, int64_t ignore_index, flce_reduction reduction, flce_dtype dt,
-                                 flce::GradLoss grad_loss, void* dH_out, void* dW_out, void* workspace,
-                                 size_t workspace_bytes, void* hip_stream, flce::Slice slice,
-                                 flce::PerRow rows = flce::PerRow{nullptr, nullptr, 0.f}) {
-  if (!H || !W || !targets || !lse || !dH_out || !dW_out) return FLCE_ERR_BAD_ARG;
-  if (!(rows.eps >= 0.f && rows.eps < 1.f)) return FLCE_ERR_BAD_ARG;
-  if (reduction != FLCE_REDUCE_MEAN && reduction != FLCE_REDUCE_SUM) return FLCE_ERR_BAD_ARG;
-  if (dt != FLCE_DTYPE_BF16 && dt != FLCE_DTYPE_F32) return FLCE_ERR_BAD_ARG;
-  flce::Plan p;
-  if (!flce::make_plan(flce::PLAN_BACKWARD, N, d, V, dt, p)) return FLCE_ERR_BAD_SHAPE;
-  if (slice.v_begin < 0 || slice.v_begin + V > slice.V_total) return FLCE_ERR_BAD_SHAPE;
-  if (!flce::aligned16(H) || !flce::aligned16(W) || !flce::aligned16(dH_out) || !flce::aligned16(dW_out))
-    return FLCE_ERR_BAD_ARG;
-  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < (size_t)p.bwd_bytes)
-    return FLCE_ERR_WORKSPACE;
-  hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  const int mean = reduction == FLCE_REDUCE_MEAN;
-  char* ws = static_cast<char*>(workspace);
-  if (dt == FLCE_DTYPE_BF16) {
-    if (p.ragged && p.tile == 128)
-      return flce::backward_t<flce::bf16_t, uint16_t, flce::SmallLoop<true>>(p, H, W, targets, lse, ignore_index, mean, grad_loss, dH_out, dW_out, ws, st, slice, rows);
-    if (p.ragged)
-      return flce::backward_t<flce::bf16_t, uint16_t, flce::FastLoop<true>>(p, H, W, targets, lse, ignore_index, mean, grad_loss, dH_out, dW_out, ws, st, slice, rows);
-    if (p.fast && p.tile == 128)
-      return flce::backward_t<flce::bf16_t, uint16_t, flce::SmallLoop<false>>(p, H, W, targets, lse, ignore_index, mean, grad_loss, dH_out, dW_out, ws, st, slice, rows);
-    if (p.fast)
-      return flce::backward_t<flce::bf16_t, uint16_t, flce::FastLoop<false>>(p, H, W, targets, lse, ignore_index, mean, grad_loss, dH_out, dW_out, ws, st, slice, rows);
-    return flce::backward_t<flce::bf16_t, uint16_t, flce::GenericLoop>(
-        p, H, W, targets, lse, ignore_index, mean, grad_loss, dH_out, dW_out, ws, st, slice, rows);
-  }
-  if (p.tile == 64)
-    return flce::backward_t<float, uint32_t, flce::F32Loop<64>>(p, H, W, targets, lse, ignore_index, mean, grad_loss, dH_out, dW_out, ws, st, slice, rows);
-  return flce::backward_t<float, uint32_t, flce::F32Loop<128>>(p, H, W, targets, lse, ignore_index, mean, grad_loss, dH_out, dW_out, ws, st, slice, rows);
-}
-
 flce_status flce_forward(const void* H, const void* W, const int64_t* targets, int64_t N, int64_t d, int64_t V,
                          int64_t ignore_index, flce_reduction reduction, flce_dtype dt, float* loss_out,
                          float* lse_out, void* workspace, size_t workspace_bytes, void* hip_stream) {
@@ -993,7 +954,7 @@ flce_status flce_backward(const void* H, const void* W, const int64_t* targets, 
                           int64_t d, int64_t V, int64_t ignore_index, flce_reduction reduction, flce_dtype dt,
                           float grad_loss, void* dH_out, void* dW_out, void* workspace, size_t workspace_bytes,
                           void* hip_stream) {
-  return backward_impl(H, W, targets, lse, N, d, V, ignore_index, reduction, dt, flce::GradLoss{grad_loss, nullptr}, dH_out,
+  return flce::backward_impl(H, W, targets, lse, N, d, V, ignore_index, reduction, dt, flce::GradLoss{grad_loss, nullptr}, dH_out,
                        dW_out, workspace, workspace_bytes, hip_stream, flce::Slice{V, 0});
 }
 
@@ -1002,7 +963,7 @@ flce_status flce_backward_device_grad(const void* H, const void* W, const int64_
                                       const float* grad_loss, void* dH_out, void* dW_out, void* workspace,
                                       size_t workspace_bytes, void* hip_stream) {
   if (!grad_loss) return FLCE_ERR_BAD_ARG;
-  return backward_impl(H, W, targets, lse, N, d, V, ignore_index, reduction, dt, flce::GradLoss{0.f, grad_loss}, dH_out,
+  return flce::backward_impl(H, W, targets, lse, N, d, V, ignore_index, reduction, dt, flce::GradLoss{0.f, grad_loss}, dH_out,
                        dW_out, workspace, workspace_bytes, hip_stream, flce::Slice{V, 0});
 }
 
@@ -1043,7 +1004,7 @@ flce_status flce_backward_rows(const void* H, const void* W, const int64_t* targ
                                float label_smoothing, flce_dtype dt, void* dH_out, void* dW_out, void* workspace,
                                size_t workspace_bytes, void* hip_stream) {
   if (!grad_rows) return FLCE_ERR_BAD_ARG;
-  return backward_impl(H, W, targets, lse, N, d, V, ignore_index, FLCE_REDUCE_SUM, dt, flce::GradLoss{1.0f, nullptr}, dH_out, dW_out,
+  return flce::backward_impl(H, W, targets, lse, N, d, V, ignore_index, FLCE_REDUCE_SUM, dt, flce::GradLoss{1.0f, nullptr}, dH_out, dW_out,
                        workspace, workspace_bytes, hip_stream, flce::Slice{V, 0},
                        flce::PerRow{nullptr, grad_rows, label_smoothing});
 }
@@ -1095,7 +1056,7 @@ flce_status flce_backward_partial(const void* H, const void* W_slice, const int6
                                   int64_t ignore_index, flce_reduction reduction, flce_dtype dt, float grad_loss,
                                   void* dH_partial_out, void* dW_slice_out, void* workspace,
                                   size_t workspace_bytes, void* hip_stream) {
-  return backward_impl(H, W_slice, targets, lse, N, d, V_slice, ignore_index, reduction, dt,
+  return flce::backward_impl(H, W_slice, targets, lse, N, d, V_slice, ignore_index, reduction, dt,
                        flce::GradLoss{grad_loss, nullptr}, dH_partial_out, dW_slice_out, workspace, workspace_bytes, hip_stream,
                        flce::Slice{V_total, v_begin});
 }

@@ -28,260 +28,10 @@
 //   slices  : the same kernels on rows [v_begin, v_begin + V) of the vocabulary
 //             (classify_target_in_slice); merge_rows_partial_kernel hands out (m, a, z_target)
 #pragma once
-#include <type_traits>
-
-#include "mainloop_f32.h"
-#include "mainloop_fast.h"
-#include "tile_mma.h"
+#include "loops.h"
+#include "recompute.h"
 
 namespace flce {
-
-// Byte offset of row block rb in a pre-tiled copy of a matrix with d columns: the block's ceil(d / 32) images of 16 KiB
-// plus a skew, so that the blocks do not start a power of two apart (the workgroups resident at one time stream
-// several dozen blocks side by side, and blocks exactly 2^k bytes apart land on the same DRAM banks).
-#ifndef FLCE_PACK_SKEW
-#define FLCE_PACK_SKEW 17408
-#endif
-__host__ __device__ __forceinline__ int64_t packed_block_offset(int rb, int d) {
-  return (int64_t)rb * ((int64_t)((d + 31) / 32 * 32) * (TILE * 2) + FLCE_PACK_SKEW);
-}
-// The same for the transposed pre-tiled copy of a matrix with `rows` rows (a multiple of 256): byte offset of the
-// block of column tile q (256 columns), which holds rows / 32 images.
-__host__ __device__ __forceinline__ int64_t packed_cols_offset(int q, int rows) {
-  return (int64_t)q * ((int64_t)rows * (TILE * 2) + FLCE_PACK_SKEW);
-}
-
-// Main-loop policies.  A kernel is written once against this interface:
-//   THREADS, MIN_WAVES (launch bounds), TILE (output tile edge), LDS (dynamic LDS bytes), WM x WN (accumulator blocks per wavefront, 16 values of a
-//   lane in one N column of ROWS rows each), Acc: a finished tile's accumulators, get(i, j, r) element r of block (i, j)
-//   (i, j, r constants after unrolling), tile_m(i, r) / tile_n(j): its position inside the tile; inside its block it is row
-//   (r / 4) QUAD + lane_row() + r % 4,
-//   slot(): which of the SLOTS lanes that share an N column this lane is,
-//   TRANSPOSING: can take an operand whose K index runs over memory rows (otherwise K-contiguous copies are made),
-//   TUNED: the bf16 loop with its persistent launches, pre-tiled copies and blocked G.
-template <int WM, int WN>
-struct VectorAcc {        // of the loops that leave the accumulators to the compiler
-  f32x16 v[WM][WN];
-  __device__ __forceinline__ float get(int i, int j, int r) const { return v[i][j][r]; }
-};
-struct GenericLoop {      // bf16 where the tuned loop does not reach (address windows); 8 wavefronts 2 x 4
-  static constexpr int TILE = flce::TILE, THREADS = flce::THREADS, WM = flce::WM, WN = flce::WN, LDS = LDS_BYTES;
-  static constexpr bool TRANSPOSING = false, TUNED = false;
-  static constexpr int MIN_WAVES = 1;
-  static constexpr int ROWS = 32, QUAD = 8, SLOTS = 4;
-  using Acc = VectorAcc<WM, WN>;
-  static __device__ __forceinline__ int lane_row() { return (threadIdx.x & 32) >> 3; }
-  static __device__ __forceinline__ int tile_m(int i, int r) { return flce::tile_m(i, r); }
-  static __device__ __forceinline__ int tile_n(int j) { return flce::tile_n(j); }
-  static __device__ __forceinline__ int slot() {
-    return ((threadIdx.x >> 6) >> 2) * 2 + ((threadIdx.x & 63) >> 5);
-  }
-  // A sequence of tiles A[a_row0 ..][:] x B[b_row0 ..][:] over K = k_elems; start() names the next tile, run() computes
-  // it and calls `released` when the next start() may come.  This loop has nothing to request ahead: start() only records the operands.
-  template <bool BT>
-  struct Stream {
-    TileSrc As, Bs;
-    int k_bytes;
-    __device__ __forceinline__ void start(const bf16_t* A, int64_t lda_bytes, int a_row0, int a_rows, const bf16_t* B,
-                                          const bf16_t*, int64_t ldb_bytes, int b_row0, int b_rows, int k_elems, char*) {
-      As = TileSrc{reinterpret_cast<const char*>(A), lda_bytes, a_row0, a_rows};
-      Bs = TileSrc{reinterpret_cast<const char*>(B), ldb_bytes, b_row0, b_rows};
-      k_bytes = k_elems * (int)sizeof(bf16_t);
-    }
-    template <typename F>
-    __device__ __forceinline__ void run(char* lds, Acc& acc, F released) {
-      tile_mainloop(As, Bs, k_bytes, lds, acc.v);
-      released();
-    }
-  };
-  static __device__ __forceinline__ void run(const void* A, int64_t lda_bytes, int a_row0, int a_rows, const void* B,
-                                             int64_t ldb_bytes, int b_row0, int b_rows, int k_bytes, char* lds,
-                                             Acc& acc) {
-    const TileSrc As{static_cast<const char*>(A), lda_bytes, a_row0, a_rows};
-    const TileSrc Bs{static_cast<const char*>(B), ldb_bytes, b_row0, b_rows};
-    tile_mainloop(As, Bs, k_bytes, lds, acc.v);
-  }
-};
-
-template <int T>
-struct F32Loop {          // fp32; T x T tiles, 4 wavefronts 2 x 2, two workgroups per CU
-  static constexpr int TILE = T, THREADS = f32::THREADS, WM = T / 64, WN = T / 64, LDS = f32::lds_bytes<T>();
-  static constexpr bool TRANSPOSING = true, TUNED = false;
-  // wavefronts per SIMD that the compiler has to leave registers for: two workgroups of 128-row tiles need it told (64-row ones have
-  // room anyway, and are 1 % faster with their sums in the accumulation registers)
-  static constexpr int MIN_WAVES = T == 128 ? 2 : 1;
-  static constexpr int ROWS = 32, QUAD = 8, SLOTS = 4;
-  using Acc = VectorAcc<WM, WN>;
-  static __device__ __forceinline__ int lane_row() { return (threadIdx.x & 32) >> 3; }
-  static __device__ __forceinline__ int tile_m(int i, int r) {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    return (wave >> 1) * (T / 2) + i * 32 + (r >> 2) * 8 + (lane >> 5) * 4 + (r & 3);
-  }
-  static __device__ __forceinline__ int tile_n(int j) {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    return (wave & 1) * (T / 2) + j * 32 + (lane & 31);
-  }
-  static __device__ __forceinline__ int slot() { return fast::slot_of_lane(); }
-  template <bool BT>
-  struct Stream {         // as GenericLoop::Stream: the other resident workgroup covers a tile's first requests
-    f32::Operand As, Bs;
-    int k_elems;
-    __device__ __forceinline__ void start(const float* A, int64_t lda_bytes, int a_row0, int a_rows, const float* B,
-                                          const float*, int64_t ldb_bytes, int b_row0, int b_rows, int k, char*) {
-      As = f32::Operand{reinterpret_cast<const char*>(A), lda_bytes, a_row0, a_rows, 0};
-      Bs = f32::Operand{reinterpret_cast<const char*>(B), ldb_bytes, b_row0, b_rows, 0};
-      k_elems = k;
-    }
-    template <typename F>
-    __device__ __forceinline__ void run(char* lds, Acc& acc, F released) {
-      f32::mainloop<T, f32::KC, f32::KC>(As, Bs, k_elems, lds, acc.v);
-      released();
-    }
-  };
-};
-
-// The tuned bf16 loop; 4 wavefronts 2 x 2 of 32 B rows x 32 B columns, global -> LDS DMA.
-// RAGGED: the hidden size is a multiple of 8 but not of 32 (the K extent of the forward and the recompute; the
-// contractions' K extents are whole tiles, they always run with the plain form).
-template <bool RAGGED, int B>
-struct TunedLoop {
-  static constexpr int TILE = 64 * B, THREADS = fast::THREADS, WM = B / 2, WN = 2 * B;
-  static constexpr bool TRANSPOSING = true, TUNED = true;
-  static constexpr int MIN_WAVES = 1;
-  static constexpr int ROWS = 64, QUAD = 16, SLOTS = 8;
-  using Acc = fast::Acc<2 * B, 2 * B>;
-  // 256-row tiles: one workgroup per CU, 4 stages of 32 KiB; 128-row tiles: two, 5 stages of 16 KiB each
-  static constexpr int PER_CU = B == 4 ? 1 : 2, STAGES = B == 4 ? fast::NS : 5, STAGE = B * 8192, LDS = STAGES * STAGE;
-  template <int LA, int LB, bool RG = false> using Pipe = fast::Pipe<LA, LB, true, B, STAGES, RG, B>;
-  // LDS that post-processing may use while the next tile's first K stages are being filled: the last stage
-  static constexpr int FREE_LDS_OFFSET = (STAGES - 1) * STAGE;
-  static __device__ __forceinline__ int lane_row() { return (threadIdx.x & 48) >> 2; }
-  static __device__ __forceinline__ int tile_m(int i, int r) {
-    const int wave = threadIdx.x >> 6;
-    return (wave >> 1) * (B * 32) + i * ROWS + (r >> 2) * QUAD + lane_row() + (r & 3);
-  }
-  static __device__ __forceinline__ int tile_n(int j) {
-    const int wave = threadIdx.x >> 6;
-    return (wave & 1) * (B * 32) + j * 16 + (threadIdx.x & 15);
-  }
-  static __device__ __forceinline__ int slot() { return (threadIdx.x >> 7) * 4 + ((threadIdx.x & 63) >> 4); }
-  // A sequence of tiles with the same B operand: start() requests the first K stages of a tile (all LDS stages must
-  // be free: every wavefront is past the previous run()), run() computes it.  BP: B is also given pre-tiled (Bp:
-  // per 256-row block and K step the 16 KiB image of its LDS tile, see pack_rows_kernel), and that copy is read.
-  template <bool BP>
-  struct Stream {
-    Pipe<fast::KC, BP ? fast::PK : fast::KC, RAGGED> pipe;
-    __device__ __forceinline__ void start(const bf16_t* A, int64_t lda_bytes, int a_row0, int a_rows, const bf16_t* Bm,
-                                          const bf16_t* Bp, int64_t ldb_bytes, int b_row0, int b_rows, int k_elems,
-                                          char* lds) {
-      const fast::Operand As{reinterpret_cast<const char*>(A), lda_bytes, a_row0, a_rows, 0};
-      if constexpr (BP) {
-        // the block's images follow each other, one per K step, 64 bytes per row
-        const fast::Operand Bs{reinterpret_cast<const char*>(Bp) + packed_block_offset(b_row0 / flce::TILE, k_elems) +
-                                   b_row0 % flce::TILE * 64, 0, 0, 0, 0};
-        pipe.start(As, Bs, k_elems, lds);
-      } else {
-        const fast::Operand Bs{reinterpret_cast<const char*>(Bm), ldb_bytes, b_row0, b_rows, 0};
-        pipe.start(As, Bs, k_elems, lds);
-      }
-    }
-    template <typename F>
-    __device__ __forceinline__ void run(char* lds, Acc& acc, F released) { pipe.run(lds, released); }
-  };
-  // A wavefront's pieces of 16 rows x (32 B) columns of bf16 on their way through its slice of the free stage, rows of
-  // ROW_BYTES in 16-byte chunks whose number is XOR-ed with mix(row), so that the 16 rows (x 2 neighbouring 8-byte halves)
-  // one write cycle touches lie in different banks, and likewise the four rows x four neighbouring chunks of a read
-  // cycle (blocks of G; output rows are read in the order of the places, and the store takes the chunks as they come).  Counted
-  // bank conflicts, of the LDS's busy cycles: recompute 3 % at 8192 x 4096 x 128256, 12 % at 4096 x 768 x 50257, dW up to 2.5 %.
-  // piece_slot: where a lane writes its 4 columns of quad rq of block i in row r; piece_chunk: where chunk c of row r is read.
-  static constexpr int ROW_BYTES = 64 * B, CHUNKS = ROW_BYTES / 16, ROWS_PER_STORE = 64 / CHUNKS;
-  static __device__ __forceinline__ int mix(int r) {
-    return B == 4 ? ((r & 3) << 2 | r >> 2) : ((r >> 1 & 1) << 2 | r >> 2);
-  }
-  static __device__ __forceinline__ int piece_slot(int r, int i, int rq) {      // chunk i * 8 + rq * 2 + (lane / 32), half (lane / 16) % 2
-    const int quarter = (threadIdx.x & 63) >> 4;
-    return r * ROW_BYTES + (((i * 8 + rq * 2 + (quarter >> 1)) ^ mix(r)) << 4) + ((quarter & 1) << 3);
-  }
-  static __device__ __forceinline__ int piece_chunk(int r, int c) { return r * ROW_BYTES + ((c ^ mix(r)) << 4); }
-};
-template <bool RAGGED> struct FastLoop : TunedLoop<RAGGED, 4> { using Even = FastLoop<false>; };
-template <bool RAGGED> struct SmallLoop : TunedLoop<RAGGED, 2> { using Even = SmallLoop<false>; };
-
-#ifndef FLCE_FWD_GROUP
-#define FLCE_FWD_GROUP 8     // row blocks per raster patch of the forward (x 32 / this many windows per XCD)
-#endif
-constexpr float LOG2E = 1.4426950408889634f;
-constexpr float NEG_INF = -__builtin_inff();
-
-// First 256 bytes of every workspace.
-struct Header {
-  int32_t status;      // 0 or FLCE_ERR_TARGET_RANGE
-  int32_t pad0;
-  int64_t n_valid;     // number of counted rows
-  float loss_sum;      // un-normalised sum of per-row losses (forward only)
-  uint32_t arrived;    // blocks of the window merge that have handed in their sums (forward only)
-};
-
-__device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
-
-// Four consecutive elements of the storage type <-> four floats.
-template <typename T> struct Pack4;
-template <> struct Pack4<float> {
-  static __device__ __forceinline__ void store(float* p, float a, float b, float c, float d) {
-    *reinterpret_cast<f32x4*>(p) = f32x4{a, b, c, d};
-  }
-  static __device__ __forceinline__ void load(const float* p, float (&v)[4]) {
-    const f32x4 x = *reinterpret_cast<const f32x4*>(p);
-    v[0] = x[0]; v[1] = x[1]; v[2] = x[2]; v[3] = x[3];
-  }
-  static __device__ __forceinline__ float one(float v) { return v; }
-};
-template <> struct Pack4<bf16_t> {
-  static __device__ __forceinline__ void store(bf16_t* p, float a, float b, float c, float d) {
-    uint2 v;
-    v.x = f32x2_to_bf16x2_bits(a, b);
-    v.y = f32x2_to_bf16x2_bits(c, d);
-    *reinterpret_cast<uint2*>(p) = v;
-  }
-  static __device__ __forceinline__ void load(const bf16_t* p, float (&v)[4]) {
-    const uint2 x = *reinterpret_cast<const uint2*>(p);
-    v[0] = __uint_as_float(x.x << 16); v[1] = __uint_as_float(x.x & 0xFFFF0000u);
-    v[2] = __uint_as_float(x.y << 16); v[3] = __uint_as_float(x.y & 0xFFFF0000u);
-  }
-  static __device__ __forceinline__ bf16_t one(float v) { return bf16_t{f32_to_bf16_bits(v)}; }
-};
-
-
-// Whether a row counts towards the loss: its target is not the ignore index and lies in
-// [0, V_total); a target outside that range that is not the ignore index is reported through `oor`.
-__device__ __forceinline__ bool target_counts(int64_t y, int64_t ignore_index, int64_t V_total, bool& oor) {
-  oor = false;
-  if (y == ignore_index) return false;
-  if (y < 0 || y >= V_total) { oor = true; return false; }
-  return true;
-}
-
-// A counted target as a column of the vocabulary slice [v_begin, v_begin + Vs) that a call works
-// on: its column inside the slice, or `outside` when it lies in another slice; -1 for rows that do
-// not count.  The whole vocabulary as the slice is v_begin = 0, Vs = V_total.
-__device__ __forceinline__ int classify_target_in_slice(int64_t y, int64_t ignore_index, int64_t V_total,
-                                                        int64_t v_begin, int Vs, int outside, bool& oor) {
-  if (!target_counts(y, ignore_index, V_total, oor)) return -1;
-  const int64_t c = y - v_begin;
-  return (c >= 0 && c < (int64_t)Vs) ? (int)c : outside;
-}
-
-// Merge of safe-softmax partials (m_k, a_k) in slot order; slots with a == 0 are
-// the identity.  Returns (M, A) with A relative to M.
-template <int S>
-__device__ __forceinline__ void merge_fixed(const float (&m)[S], const float (&a)[S], float& M, float& A) {
-  M = NEG_INF;
-#pragma unroll
-  for (int s = 0; s < S; ++s) if (a[s] > 0.f) M = fmaxf(M, m[s]);
-  A = 0.f;
-#pragma unroll
-  for (int s = 0; s < S; ++s) if (a[s] > 0.f) A += a[s] * fast_exp2((m[s] - M) * LOG2E);
-}
 
 // ------------------------------------------------------------------------------------
 // Forward tiles.  A = W tile (M = vocabulary, inside a lane), B = H tile (N = tokens,
@@ -428,14 +178,6 @@ __global__ __launch_bounds__(L::THREADS, L::MIN_WAVES) void fwd_tiles_kernel(
   }
 }
 
-// Sum over the 64 lanes of a wavefront in a fixed tree (every lane gets it).
-template <typename V>
-__device__ __forceinline__ V wave_sum(V v) {
-#pragma unroll
-  for (int s = 32; s > 0; s >>= 1) v += __shfl_xor(v, s, 64);
-  return v;
-}
-
 // The partials (m, a, z_target) of a row's `n_parts` windows or vocabulary slices, merged (part k of row n at
 // pm[k * stride + n], likewise pa, pz).  A block has ROWS rows x GROUPS threads; group g takes a contiguous run of the
 // parts, U of them at a time with all their loads in flight together (a part past the end re-reads the last one and is
@@ -486,49 +228,6 @@ __device__ __forceinline__ void merge_parts(const float* __restrict__ pm, const 
       for (int k = 0; k < GROUPS; ++k) { gm[k] = sm[k][t]; ga[k] = sa[k][t]; z += sz[k][t]; }
       merge_fixed<GROUPS>(gm, ga, M, A);
     }
-  }
-}
-
-// Where the reduced loss of a call goes.
-struct LossOut {
-  float* blk_loss; int* blk_cnt; int* blk_oor;      // one entry per block of the merge
-  Header* hdr; float* loss; int mean;
-  int32_t* status; int64_t* n_valid;                // the caller's own words, or null
-};
-
-// The call's loss, by one thread: normalisation, header.
-__device__ __forceinline__ void write_loss(const LossOut& o, double total, int64_t nv, int any) {
-  double loss = total;
-  if (o.mean) loss = nv > 0 ? total / (double)nv : 0.0;
-  o.hdr->status = any ? 4 : 0;
-  o.hdr->pad0 = 0;
-  o.hdr->n_valid = nv;
-  o.hdr->loss_sum = (float)total;
-  *o.loss = (float)loss;
-  if (o.status) *o.status = any ? 4 : 0;
-  if (o.n_valid) *o.n_valid = nv;
-}
-
-// The second half of the reduction, by one block: fixed-order fp64 sum of the per-block partials.
-__device__ __forceinline__ void finalize_loss(const LossOut& o, int n_blk) {
-  __shared__ double sl[16];
-  __shared__ long long sc[16];
-  __shared__ int so[16];
-  double l = 0.0; long long c = 0; int bad = 0;
-  for (int b = threadIdx.x; b < n_blk; b += blockDim.x) {
-    // (written by other blocks of this launch when the merge calls this: read past this XCD's own caches)
-    l += (double)__hip_atomic_load(o.blk_loss + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    c += __hip_atomic_load(o.blk_cnt + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    bad |= __hip_atomic_load(o.blk_oor + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  }
-  l = wave_sum(l); c = wave_sum(c); bad = __ballot(bad != 0) != 0ull;
-  const int wave = threadIdx.x >> 6, n_waves = blockDim.x >> 6;
-  if ((threadIdx.x & 63) == 0) { sl[wave] = l; sc[wave] = c; so[wave] = bad; }
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    double total = 0.0; long long nv = 0; int any = 0;
-    for (int w = 0; w < n_waves; ++w) { total += sl[w]; nv += sc[w]; any |= so[w]; }
-    write_loss(o, total, nv, any);
   }
 }
 
@@ -600,20 +299,6 @@ __global__ __launch_bounds__(ROWS * GROUPS) void merge_rows_kernel(
 }
 
 __global__ __launch_bounds__(256) void finalize_loss_kernel(LossOut o, int n_blk) { finalize_loss(o, n_blk); }
-
-// 16 bytes of the storage type as floats.
-template <typename T>
-struct Vec16 {
-  static constexpr int N = 16 / (int)sizeof(T);
-  static __device__ __forceinline__ void load(const T* p, float (&v)[N]) {
-    const u32x4 x = *reinterpret_cast<const u32x4*>(p);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if constexpr (sizeof(T) == 2) { v[2 * e] = __uint_as_float(x[e] << 16); v[2 * e + 1] = __uint_as_float(x[e] & 0xFFFF0000u); }
-      else v[e] = __uint_as_float(x[e]);
-    }
-  }
-};
 
 // mean_v Z_iv = H_i . (sum_v W_v) / V, for label smoothing: the column sums of W in two fixed-order
 // steps (1024-row chunks, then the chunks in order), then one dot product per row.
@@ -1007,253 +692,6 @@ __global__ __launch_bounds__(256) void transpose_pad_kernel(const U* __restrict_
 }
 
 // ------------------------------------------------------------------------------------
-// Backward, step 1 (on the compacted rows): logit tile recomputed exactly as in the
-// forward (the same products added up in the same order; fp32 on the same tile edge, see plan_base), then
-//   g = exp(z - lse_row) - [v == y_row]            (unscaled; Gamma comes later)
-// rounded to T and written to the staging tile
-//   G [row - chunk_n0][vocab - chunk_v0]   (ldG  elements per row; with the tuned loop in blocks of 16 rows x 32
-//                                           positions of 1 KiB, ldG = BYTES from one group of 16 rows to the next)
-// and, for main loops that need K-contiguous operands, also transposed:
-//   GT[vocab - chunk_v0][row - chunk_n0]   (ldGT elements per row)
-// Padded vocabulary columns and the padding rows behind the last counted row are 0.
-// Tiles that lie entirely behind the last counted row return at once; the
-// contractions never read them.
-// ------------------------------------------------------------------------------------
-template <typename T>
-struct RecomputeArgs {
-  const T* Hc; const T* HcT; const T* W; const int* tgt_c; const float* lse_c; const Header* hdr;
-  int npad, d, V, nt0, n_nt, vt0, n_vt;
-  T* G; int64_t ldG; T* GT; int64_t ldGT;
-  // per-row variant only: upstream gradient of each compact row, label-smoothing constants
-  const float* gam_c; float onehot_weight; float uniform_part;   // 1 - eps, eps / V
-};
-
-// Per-row inputs of a recompute tile, one set per token column a lane owns.
-template <typename L>
-struct RowMeta {
-  int tgt[L::WN];       // target column inside the slice, -1 for a padding row
-  float lse[L::WN];
-  float gam[L::WN];     // per-row variant only
-};
-
-// The recompute step.  With the tuned loop the launch has at most one round of workgroups (NUM_CU * L::PER_CU: 256 with
-// 256-row tiles, 512 with 128-row ones) and workgroup b takes tiles b, b + gridDim.x, ... of the chunk; with the other loops
-// it has one per tile.  With the tuned loop the first K stages of a workgroup's next tile (and that tile's per-row inputs) are
-// requested before the current tile's G is formed and stored, so the latency of a tile's first operands hides behind
-// the previous tile's post-processing: it matters when the K loop is short (small d).
-// PER_ROW: g = Gamma_row * (p - (1 - eps) [v == y_row] - eps / V), the upstream gradient applied here because
-// it differs from row to row (Alg. 2 with a per-position Gamma); otherwise g = p - [v == y_row] and the
-// scalar Gamma is applied when the contractions write out.
-template <typename T, typename L, bool HKR, bool PER_ROW = false>
-__global__ __launch_bounds__(L::THREADS, L::MIN_WAVES) void recompute_kernel(RecomputeArgs<T> a) {
-  extern __shared__ __align__(16) char lds[];
-  const T* __restrict__ Hc = a.Hc; const T* __restrict__ HcT = a.HcT; const T* __restrict__ W = a.W;
-  const int npad = a.npad, d = a.d, V = a.V;
-  T* __restrict__ G = a.G; T* __restrict__ GT = a.GT; const int64_t ldG = a.ldG, ldGT = a.ldGT;
-  // Only the row tiles that hold counted rows are rastered (their number is known on the device
-  // alone), so the XCDs share the work evenly however many rows are ignored; workgroups beyond the
-  // useful tiles of a launch sized for N rows leave at once.
-  const int n_nt = max(0, min(a.n_nt, ((int)a.hdr->n_valid - a.nt0 * L::TILE + L::TILE - 1) / L::TILE));
-  const int useful = n_nt * a.n_vt;
-  int t = blockIdx.x;
-  if (t >= useful) return;
-  const int64_t ld_bytes = (int64_t)d * sizeof(T);
-  auto place = [&](int tile, int& p, int& q) {     // row tile, vocabulary tile inside the chunk
-    grouped_raster(xcd_contiguous_id(tile, useful), n_nt, a.n_vt, 8, p, q);
-  };
-  auto load_meta = [&](int n0, RowMeta<L>& m) {
-#pragma unroll
-    for (int j = 0; j < L::WN; ++j) {
-      const int n = n0 + L::tile_n(j);
-      m.tgt[j] = a.tgt_c[n];
-      m.lse[j] = a.lse_c[n];
-      if constexpr (PER_ROW) m.gam[j] = a.gam_c[n];
-    }
-  };
-  // Marks the point where a tile's per-row inputs must have arrived: the compiler's wait for them lands here (it
-  // cannot see the main loop's own requests, so a wait placed later would also wait for the next tile's operands).
-  auto need_meta = [&](RowMeta<L>& m) {
-#pragma unroll
-    for (int j = 0; j < L::WN; ++j) {
-      asm volatile("" : "+v"(m.tgt[j]), "+v"(m.lse[j]));
-      if constexpr (PER_ROW) asm volatile("" : "+v"(m.gam[j]));
-    }
-  };
-  typename L::template Stream<HKR> stream;
-  int p, q;
-  place(t, p, q);
-  RowMeta<L> meta;
-  if constexpr (L::TUNED) load_meta((a.nt0 + p) * L::TILE, meta);
-  stream.start(W, ld_bytes, (a.vt0 + q) * L::TILE, V, Hc, HcT, ld_bytes, (a.nt0 + p) * L::TILE, npad, d, lds);
-  typename L::Acc acc;
-  for (;;) {
-    const int t_next = t + gridDim.x;
-    // (a main loop with nothing to request ahead gets one tile per workgroup)
-    const bool more = L::TUNED && t_next < useful;
-    int p_next = 0, q_next = 0;
-    RowMeta<L> meta_next;
-    stream.run(lds, acc, [&] {
-      if constexpr (!L::TUNED) load_meta((a.nt0 + p) * L::TILE, meta);   // no registers to spare across that main loop
-      need_meta(meta);
-      if (more) {
-        place(t_next, p_next, q_next);
-        load_meta((a.nt0 + p_next) * L::TILE, meta_next);
-        stream.start(W, ld_bytes, (a.vt0 + q_next) * L::TILE, V, Hc, HcT, ld_bytes, (a.nt0 + p_next) * L::TILE, npad, d, lds);
-      }
-    });
-
-    const int v0 = (a.vt0 + q) * L::TILE;
-    if constexpr (L::TUNED) {
-      // Tuned loop.  A lane holds, of 16 token rows x (32 B) vocabulary positions per j, scattered 8-byte pieces of one
-      // row; stored as they lie, every store instruction would touch 16 different memory rows in 32-byte pieces.  Each wavefront
-      // therefore passes its piece (4 KiB of bf16 with 256-row tiles) through its own slice of the free LDS stage and
-      // writes whole blocks of G, 1 KiB of consecutive bytes per instruction.
-      static_assert(sizeof(T) == 2, "the tuned epilogue is laid out for bf16");
-      constexpr int POS = L::WM * L::ROWS;                        // vocabulary positions of a piece
-      const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-      char* stage = lds + L::FREE_LDS_OFFSET + wave * (16 * L::ROW_BYTES);
-      const int wrow = lane & 15;                                 // writer: token row of the piece
-      const int rrow = lane >> 2, rchunk = lane & 3;              // reader: row and 16-byte chunk inside a block
-      const int vbase = v0 + (wave >> 1) * POS;                   // first vocabulary position of the piece
-#pragma unroll
-      for (int j = 0; j < L::WN; ++j) {
-        const int tgt = meta.tgt[j];
-        // exp(z - lse) = 2^(z * log2e - lse * log2e); a padding row (tgt < 0) gets lse = +inf here, so its p is
-        // exactly 0, and no column equals its target: its row of G is 0 without a mask
-        const float ll = tgt >= 0 ? -meta.lse[j] * LOG2E : NEG_INF;
-        float gam = 1.f;
-        if constexpr (PER_ROW) gam = tgt >= 0 ? meta.gam[j] : 0.f;
-        const float unif = tgt >= 0 ? a.uniform_part : 0.f;
-        // A whole column of blocks without a target of the wavefront and inside the vocabulary (almost all are: POS of V
-        // positions) needs no tests (step of 4326 x 232 x 74697 1044 -> 1008 us, 1144 x 576 x 191782 1306 -> 1264,
-        // 4096 x 768 x 50257 1198 -> 1178).
-        if (vbase + POS <= V && __ballot((unsigned)(tgt - vbase) < (unsigned)POS) == 0ull) {
-#pragma unroll
-          for (int i = 0; i < L::WM; ++i) {
-#pragma unroll
-            for (int rq = 0; rq < 4; ++rq) {
-              float g[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                g[e] = fast_exp2(fmaf(acc.get(i, j, rq * 4 + e), LOG2E, ll));
-                if constexpr (PER_ROW) g[e] = gam * (g[e] - unif);
-              }
-              uint2 packed;
-              packed.x = f32x2_to_bf16x2_bits(g[0], g[1]);
-              packed.y = f32x2_to_bf16x2_bits(g[2], g[3]);
-              *reinterpret_cast<uint2*>(stage + L::piece_slot(wrow, i, rq)) = packed;
-            }
-            __builtin_amdgcn_sched_barrier(0);   // one accumulator block at a time in VGPRs
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < L::WM; ++i) {
-            const int blk0 = vbase + i * L::ROWS;                   // wave-uniform
-            const bool whole = blk0 + L::ROWS <= V;
-            // Does any token column of this wavefront have its target among the block's vocabulary positions?
-            // Almost never, and then the one-hot term costs nothing: a wave-uniform branch.
-            const bool hit = __ballot((unsigned)(tgt - blk0) < (unsigned)L::ROWS) != 0ull;
-#pragma unroll
-            for (int rq = 0; rq < 4; ++rq) {
-              const int vpos = blk0 + rq * L::QUAD + L::lane_row();   // first of this lane's 4 consecutive positions
-              float g[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) g[e] = fast_exp2(fmaf(acc.get(i, j, rq * 4 + e), LOG2E, ll));
-              if (hit) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  if (vpos + e == tgt) g[e] -= PER_ROW ? a.onehot_weight : 1.f;
-              }
-              if constexpr (PER_ROW) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) g[e] = gam * (g[e] - unif);
-              }
-              if (!whole) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  if (vpos + e >= V) g[e] = 0.f;
-              }
-              uint2 packed;
-              packed.x = f32x2_to_bf16x2_bits(g[0], g[1]);
-              packed.y = f32x2_to_bf16x2_bits(g[2], g[3]);
-              *reinterpret_cast<uint2*>(stage + L::piece_slot(wrow, i, rq)) = packed;
-            }
-            __builtin_amdgcn_sched_barrier(0);   // one accumulator block at a time in VGPRs
-          }
-        }
-        // the piece is complete in LDS (a wavefront's LDS operations complete in order): write it out, a block at a
-        // time.  G is stored in blocks of 16 rows x 32 positions (1 KiB; the blocks of a row
-        // group along the vocabulary, row groups ldG BYTES apart), so that both contractions fetch whole blocks.
-        const int row0 = p * L::TILE + (wave & 1) * (L::WN * 16) + j * 16;          // a row group
-        char* __restrict__ gdst = reinterpret_cast<char*>(G) + (int64_t)(row0 >> 4) * ldG +
-                                  (int64_t)(q * (L::TILE / 32) + (wave >> 1) * (POS / 32)) * 1024 + lane * 16;
-#pragma unroll
-        for (int k = 0; k < POS / 32; ++k)
-          *reinterpret_cast<u32x4*>(gdst + k * 1024) = *reinterpret_cast<const u32x4*>(stage + L::piece_chunk(rrow, k * 4 + rchunk));
-      }
-    } else {
-    // Blocks in (i, j) order, i outermost: what depends on the vocabulary position only (the padding masks of a
-    // block that straddles the vocabulary's end) is then shared by the four j of one i and dies with it.
-#pragma unroll
-    for (int i = 0; i < L::WM; ++i) {
-      // All 32 vocabulary positions of a block belong to one wavefront: "behind the vocabulary's end" and
-      // "straddles the end" are wave-uniform tests, and only a straddling block masks single elements.
-      const int blk0 = v0 + __builtin_amdgcn_readfirstlane(L::tile_m(i, 0) & ~31);
-      const bool whole = blk0 + 32 <= V;
-#pragma unroll
-      for (int j = 0; j < L::WN; ++j) {
-        const int nl = p * L::TILE + L::tile_n(j);       // row inside the staging tile
-        // this lane's first position in the row; block (i, rq) lies a constant 32 i + 8 rq further on
-        T* __restrict__ grow = G + (int64_t)nl * ldG + q * L::TILE + L::tile_m(0, 0);
-        const int tgt = meta.tgt[j];
-        // exp(z - lse) = 2^(z * log2e - lse * log2e); a padding row (tgt < 0) gets lse = +inf here, so its p is
-        // exactly 0, and no column equals its target: its row of G is 0 without a mask
-        const float ll = tgt >= 0 ? -meta.lse[j] * LOG2E : NEG_INF;
-        float gam = 1.f;
-        if constexpr (PER_ROW) gam = tgt >= 0 ? meta.gam[j] : 0.f;
-        const float unif = tgt >= 0 ? a.uniform_part : 0.f;
-        // Does any token column of this wavefront have its target among the block's 32 vocabulary positions?
-        // Almost never (32 of V positions), and then the one-hot term costs nothing: a wave-uniform branch.
-        const bool hit = __ballot((unsigned)(tgt - blk0) < 32u) != 0ull;
-#pragma unroll
-        for (int rq = 0; rq < 4; ++rq) {
-          const int mloc = L::tile_m(i, rq * 4);    // first of 4 consecutive vocabulary positions
-          float g[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) g[e] = fast_exp2(fmaf(acc.get(i, j, rq * 4 + e), LOG2E, ll));
-          if (hit) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (v0 + mloc + e == tgt) g[e] -= PER_ROW ? a.onehot_weight : 1.f;
-          }
-          if constexpr (PER_ROW) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) g[e] = gam * (g[e] - unif);
-          }
-          if (!whole) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (v0 + mloc + e >= V) g[e] = 0.f;
-          }
-          const int vl = q * L::TILE + mloc;
-          Pack4<T>::store(grow + (i * 32 + rq * 8), g[0], g[1], g[2], g[3]);
-          if constexpr (!L::TRANSPOSING) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) GT[(int64_t)(vl + e) * ldGT + nl] = Pack4<T>::one(g[e]);
-          }
-        }
-        __builtin_amdgcn_sched_barrier(0);   // one 32x32 block at a time in VGPRs
-      }
-    }
-    }
-    if (!more) break;
-    need_meta(meta_next);
-    t = t_next; p = p_next; q = q_next;
-    meta = meta_next;
-  }
-}
-
-// ------------------------------------------------------------------------------------
 // Backward, step 2: out[n][m] (+)= sum_k A[m][k] * B[n][k]
 //   dH: A = W^T chunk [d][Vc], B = G  [rows][Vc]   (contraction over the vocabulary chunk)
 //   dW: A = Hc^T      [d][Nc], B = GT [vocab][Nc]  (contraction over the compact-row chunk)
@@ -1277,12 +715,6 @@ enum : int { READ_ACC = 1, WRITE_ACC = 2, WRITE_OUT = 4, ROWS_COMPACT = 8, K_COM
 //   OPS_DH_F32 : fp32; A = W rows of the vocabulary chunk [k][m], B = G row-major [n][k]
 //   OPS_DW_F32 : fp32; A = Hc rows of the row chunk [k][m], B = G row-major [k][n] (K over the rows of both)
 enum : int { OPS_KC = 0, OPS_DH_TR = 1, OPS_DW_TR = 2, OPS_DH_F32 = 3, OPS_DW_F32 = 4 };
-
-// Upstream gradient of the scalar loss: a device word if there is one, a host value otherwise.
-struct GradLoss {
-  float value; const float* word;
-  __device__ __forceinline__ float get() const { return word ? *word : value; }
-};
 
 template <typename T>
 struct ContractArgs {

@@ -8,8 +8,18 @@ tensors, names the stream and chains the autograd graph.
 
 H is [..., d] (leading dimensions are flattened to N rows), W is [V, d], both bf16 or both fp32, contiguous, on the
 same GPU; targets are int64 with the leading shape of H.  The N x V logits are never formed.
+
+On a few logits per row:
+
+    logits, ids, lse = linear_topk(H, W, k)                           # the k largest of each row
+    loss = linear_distillation(H, W, ids, logits, temperature=2.0)    # a student on a teacher's lists
+    scores, tokens, parents, finished = beam_step(H, W, scores, finished, eos_id=2)
+    reorder_states(parents, cache, out=cache)                         # the beams' states follow
 """
 from __future__ import annotations
+
+import contextlib
+import weakref
 
 import torch
 
@@ -147,3 +157,223 @@ def linear_cross_entropy(H, W, targets, ignore_index=-100, reduction="mean", lab
             raise ValueError("label smoothing is available with reduction='none' only")
         return _ScalarLoss.apply(H, W, targets, int(ignore_index), reduction)
     return _RowLosses.apply(H, W, targets, int(ignore_index), float(label_smoothing))
+
+
+def _on_device(device):
+    """The library launches on the current device: the tensors' own, whichever is current for the caller."""
+    return contextlib.nullcontext() if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+
+def _operands(H, W):
+    if H.dtype not in _DT or W.dtype != H.dtype:
+        raise TypeError("H and W must both be bfloat16 or both float32")
+    if not (H.is_cuda and W.is_cuda):
+        raise ValueError("libflce works on GPU tensors only")
+    if H.device != W.device:
+        raise ValueError("H and W are on different devices")
+    if H.dim() < 1 or W.dim() != 2 or W.shape[1] != H.shape[-1]:
+        raise ValueError("shapes: H [..., d], W [V, d]")
+    return H.reshape(-1, H.shape[-1]).contiguous(), W.contiguous()
+
+
+def _beside(H, dtype, **tensors):
+    """Further arguments as the library wants them: H's device, contiguous, of one type."""
+    for name, t in tensors.items():
+        if t.device != H.device:
+            raise ValueError(f"{name} is on another device than H")
+        yield t.to(dtype).contiguous()
+
+
+def _scratch(nbytes, device, what):
+    if nbytes == 0:
+        raise ValueError(f"unsupported shape ({what})")
+    return torch.empty(nbytes, dtype=torch.uint8, device=device), nbytes
+
+
+def linear_topk(H, W, k):
+    """The k largest logits of each row of H . W^T, in descending order (equal ones by id), without the logits tensor.
+
+    Returns (logits [..., k] float32, ids [..., k] int64, lse [...] float32); lse is the log-sum-exp over the whole
+    vocabulary, so logits - lse[..., None] are log-probabilities.  1 <= k <= 256.  Not differentiable.
+    """
+    with torch.no_grad():
+        H2, W2 = _operands(H.detach(), W.detach())
+        (N, d), V, dt, dev = H2.shape, W2.shape[0], _DT[H2.dtype], H2.device
+        k = int(k)
+        ws, nb = _scratch(B.flce_topk_workspace_bytes(N, d, V, k, dt), dev,
+                          "d must be a multiple of 8, 1 <= k <= min(256, V), V <= 2^22, at least one row")
+        logits = torch.empty(N, k, dtype=torch.float32, device=dev)
+        ids = torch.empty(N, k, dtype=torch.int64, device=dev)
+        lse = torch.empty(N, dtype=torch.float32, device=dev)
+        with _on_device(dev):
+            _check(B.flce_topk(H2, W2, N, d, V, k, dt, logits, ids, lse, ws, nb, _stream(dev)))
+    lead = H.shape[:-1]
+    return logits.reshape(*lead, k), ids.reshape(*lead, k), lse.reshape(lead)
+
+
+class _EagerGraph:
+    """Lives as long as the autograd graph of an eager distillation does."""
+
+    def __init__(self, leaves):
+        self.leaves = [weakref.ref(t) for t in leaves]
+
+
+_eager_graphs = weakref.WeakSet()
+
+
+def _graph_of(H, W):
+    """While an autograd graph made outside a HIP graph's capture lives, torch's gradient accumulators of its leaves belong to the
+    stream it was made on; a backward captured for the same leaves would wait for that stream, which ends the process.  Such a
+    capture is refused."""
+    leaves = [t for t in (H, W) if t.requires_grad and t.is_leaf]
+    if not leaves or not torch.is_grad_enabled():
+        return None
+    if torch.cuda.is_available() and torch.cuda.is_current_stream_capturing():
+        if any(r() is t for g in _eager_graphs for r in g.leaves for t in leaves):
+            raise RuntimeError("an eager distillation of the same H or W is alive: drop its loss before capturing another")
+        return None
+    graph = _EagerGraph(leaves)
+    _eager_graphs.add(graph)
+    return graph
+
+
+class _Distillation(torch.autograd.Function):
+    """Loss over a teacher's lists; mean or sum over the rows that count, or one loss per row."""
+
+    @staticmethod
+    def forward(ctx, H, W, ids, logits, temperature, reduction, graph):
+        H2, W2 = _operands(H, W)
+        (N, d), V, dt, dev = H2.shape, W2.shape[0], _DT[H2.dtype], H2.device
+        K = ids.shape[-1]
+        ids2, = _beside(H2, torch.int64, teacher_ids=ids.reshape(-1, K))
+        t2, = _beside(H2, torch.float32, teacher_logits=logits.reshape(-1, K))
+        ws, nb = _scratch(B.flce_distill_workspace_bytes(N, d, V, K, dt, 0), dev,
+                          "d must be a multiple of 8, 1 <= K <= 256, at least one row")
+        rows = reduction == "none"
+        out = torch.empty(N if rows else (), dtype=torch.float32, device=dev)
+        lse = torch.empty(N, dtype=torch.float32, device=dev)
+        zt = torch.empty(N, K, dtype=torch.float32, device=dev)
+        with _on_device(dev):
+            _check(B.flce_distill_forward(H2, W2, ids2, t2, N, d, V, K, temperature, _RED.get(reduction, B.FLCE_REDUCE_SUM), dt,
+                                          None if rows else out, out if rows else None, lse, zt, ws, nb, _stream(dev)))
+        ctx.save_for_backward(H2, W2, ids2, t2, lse, zt)
+        ctx.meta = (H.shape, temperature, reduction)
+        ctx.graph = graph
+        return out.reshape(H.shape[:-1]) if rows else out
+
+    @staticmethod
+    def backward(ctx, grad):
+        H2, W2, ids2, t2, lse, zt = ctx.saved_tensors
+        shape, temperature, reduction = ctx.meta
+        (N, d), V, K, dt, dev = H2.shape, W2.shape[0], ids2.shape[1], _DT[H2.dtype], H2.device
+        # The kernels read the gradient where it is; one that is only marked as negated or zero is made first.
+        g = grad.to(device=dev, dtype=torch.float32)
+        if g.is_neg() or g._is_zerotensor():
+            g = g.clone().resolve_neg()
+        rows = reduction == "none"
+        if rows:
+            g = g.reshape(-1).contiguous()
+        dH = torch.empty_like(H2)
+        dW = torch.empty_like(W2)
+        ws, nb = _scratch(B.flce_distill_workspace_bytes(N, d, V, K, dt, 1), dev, "as in the forward")
+        with _on_device(dev):
+            _check(B.flce_distill_backward(H2, W2, ids2, t2, lse, zt, N, d, V, K, temperature, _RED.get(reduction, B.FLCE_REDUCE_SUM),
+                                           dt, None if rows else g, g if rows else None, dH, dW, ws, nb, _stream(dev)))
+        return dH.reshape(shape), dW, None, None, None, None, None
+
+
+def linear_distillation(H, W, teacher_ids, teacher_logits, temperature=1.0, reduction="mean"):
+    """Distillation of softmax(H . W^T) from a teacher's largest logits, without the logits tensor.
+
+    teacher_ids [..., K] (int64, negative: no entry) and teacher_logits [..., K] (float, no gradient) with the leading shape
+    of H, K <= 256, as linear_topk gives them.  Per row T^2 KL(p || q) with p = softmax over the list's logits / T and q = softmax over
+    the vocabulary's logits / T, T = temperature.  reduction: "mean" (over the rows that have an entry), "sum" or "none".
+    Rows without an entry, and rows with an id beyond the vocabulary, have loss and gradient 0.
+
+    Forward and backward can be captured into a HIP graph while no autograd graph made outside of it holds H or W as a leaf.
+    """
+    if reduction not in ("mean", "sum", "none"):
+        raise ValueError("reduction must be 'mean', 'sum' or 'none'")
+    if teacher_ids.dtype.is_floating_point or not teacher_logits.dtype.is_floating_point:
+        raise TypeError("teacher_ids are integers, teacher_logits are floating point")
+    if teacher_ids.shape != teacher_logits.shape or teacher_ids.dim() != H.dim() or teacher_ids.shape[:-1] != H.shape[:-1]:
+        raise ValueError("shapes: H [..., d], teacher_ids and teacher_logits [..., K]")
+    return _Distillation.apply(H, W, teacher_ids, teacher_logits.detach(), float(temperature), reduction, _graph_of(H, W))
+
+
+def beam_step(H, W, scores, finished=None, n_out=None, eos_id=-1, pad_id=0):
+    """One step of a beam search on softmax(H . W^T), without the logits tensor.
+
+    H [batch, beams, d], scores [batch, beams] (sums of log-probabilities), finished [batch, beams] (bool) or None.  Returns the
+    n_out (default: beams) best continuations of each search in order: scores [batch, n_out] float32, tokens and parents
+    (the beam each comes from) int64, finished bool.  A finished beam stays a candidate with its score and `pad_id`.
+    """
+    if H.dim() != 3 or scores.shape != H.shape[:2] or (finished is not None and finished.shape != H.shape[:2]):
+        raise ValueError("shapes: H [batch, beams, d], scores and finished [batch, beams]")
+    with torch.no_grad():
+        H2, W2 = _operands(H.detach(), W.detach())
+        (batch, beams, d), V, dt, dev = H.shape, W2.shape[0], _DT[H2.dtype], H2.device
+        n_out = beams if n_out is None else int(n_out)
+        s, = _beside(H2, torch.float32, scores=scores.detach())
+        f = None
+        if finished is not None:
+            f, = _beside(H2, torch.bool, finished=finished)
+        ws, nb = _scratch(B.flce_beam_workspace_bytes(batch, beams, d, V, n_out, dt), dev,
+                          "d must be a multiple of 8, beams and n_out 1 .. 64, V <= 2^22, at least one search")
+        out = (torch.empty(batch, n_out, dtype=torch.float32, device=dev), torch.empty(batch, n_out, dtype=torch.int64, device=dev),
+               torch.empty(batch, n_out, dtype=torch.int64, device=dev), torch.empty(batch, n_out, dtype=torch.bool, device=dev))
+        with _on_device(dev):
+            _check(B.flce_beam_step(H2, W2, s, f, batch, beams, d, V, n_out, int(eos_id), int(pad_id), dt, *out, ws, nb, _stream(dev)))
+    return out
+
+
+def reorder_states(parents, states, out=None, dim=1, status=None):
+    """The beams' states after a step: out[..., b, j, ...] = states[..., b, parents[b, j], ...].
+
+    parents [batch, beams_out] (int64); dimension `dim` of `states` is the batch, the next one the beams; what lies ahead of it
+    (layers, keys and values) may be strided once, a beam's row is contiguous.  out: a tensor of states' shape with beams_out
+    beams (a new one by default); out=states reorders in place (up to 16 beams).  status: an int32 tensor that becomes
+    FLCE_ERR_TARGET_RANGE where a parent is no beam (whose row is left as it was).  Returns out.
+    """
+    if not states.is_cuda or parents.device != states.device or (out is not None and out.device != states.device):
+        raise ValueError("parents, states and out must be on one GPU")
+    if parents.dim() != 2 or states.dim() < dim + 2 or dim < 0 or states.shape[dim] != parents.shape[0]:
+        raise ValueError("shapes: parents [batch, beams_out], states [..., batch, beams, ...] with the batch at `dim`")
+    if status is not None and (status.dtype is not torch.int32 or status.device != states.device or status.numel() != 1):
+        raise TypeError("status is one int32 on the states' GPU")
+    batch, beams_out = parents.shape
+    beams_in = states.shape[dim + 1]
+    want = states.shape[:dim + 1] + (beams_out,) + states.shape[dim + 2:]
+    if out is None:
+        out = torch.empty(want, dtype=states.dtype, device=states.device)
+    if out.shape != want or out.dtype != states.dtype:
+        raise ValueError("out does not have the shape and type of the reordered states")
+    if out.numel() == 0:
+        return out
+
+    def strides(t):
+        """Bytes from row to row and from outer to outer."""
+        size, run = t.element_size(), 1
+        for n, s in zip(reversed(t.shape[dim + 2:]), reversed(t.stride()[dim + 2:])):
+            if n > 1 and s != run:
+                raise ValueError("a beam's state must be contiguous")
+            run *= n
+        row = t.stride(dim + 1) if t.shape[dim + 1] > 1 else (t.stride(dim) if batch > 1 else run)
+        if batch > 1 and t.stride(dim) != t.shape[dim + 1] * row:
+            raise ValueError("batch and beams must be one run of rows")
+        outer, step = 1, None
+        for n, s in zip(reversed(t.shape[:dim]), reversed(t.stride()[:dim])):
+            if n > 1:
+                if step is not None and s != step * outer:
+                    raise ValueError("the dimensions ahead of the batch must be strided once")
+                step = s if step is None else step
+                outer *= n
+        return run * size, outer, row * size, (step or 0) * size
+
+    row_bytes, outer, src_row, src_outer = strides(states)
+    _, _, dst_row, dst_outer = strides(out)
+    p = parents.to(torch.int64).contiguous()
+    with _on_device(states.device):
+        _check(B.flce_beam_reorder(states, out, p, outer, batch, beams_in, beams_out, row_bytes, src_row, src_outer, dst_row, dst_outer,
+                                   status, _stream(states.device)))
+    return out
