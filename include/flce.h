@@ -348,8 +348,8 @@ flce_status flce_topk(const void* H, const void* W, int64_t N, int64_t d, int64_
  *   grad_loss     : device, 1 float, the upstream gradient of the scalar loss, or NULL;
  *   grad_rows     : device, N floats, of the losses per row (sum semantics), or NULL: exactly one of the two.
  * G = dloss/dZ is rounded to `dt` before the two contractions, as flce_backward's and flce_backward_rows' is.
- * Workspaces: flce_distill_workspace_bytes(N, d, V, K, dt, for_backward) bytes, 0 for an invalid shape.  Forward: 8 bytes per 64
- * (fp32: 32) logits of a chunk of rows (up to 256 MiB or 256 rows), the lists by tile, flce_forward's copy of H; backward:
+ * Workspaces: flce_distill_workspace_bytes(N, d, V, K, dt, for_backward) bytes, 0 for an invalid shape.  Forward: 8 bytes per window
+ * and row, the lists by tile (4 bytes per entry, and per pair of a row and a vocabulary tile), flce_forward's copy of H; backward:
  * flce_backward's and 4 bytes per list entry.
  */
 size_t flce_distill_workspace_bytes(int64_t N, int64_t d, int64_t V, int64_t K, flce_dtype dt, int for_backward);

@@ -4,11 +4,17 @@
 //   d loss / d z_v = T (exp(z_v / T - lse) - sum of p_k with id_k = v)
 // An entry with a negative id is absent, one whose logit is -inf has no share; a row without a share does not count.
 #pragma once
-#include "logit_tiles.h"
+#include "plan.h"
+#include "recompute.h"
 
 namespace flce {
 
 constexpr int DISTILL_MAX = 256;          // entries of a list
+// A listed logit of a tile: token row in the tile (bits 0-7), vocabulary position in the tile (8-15), place in the row's list (16-23).
+constexpr uint32_t NO_ENTRY = 0xFFFFFFFFu;
+__host__ __device__ __forceinline__ constexpr uint32_t list_entry(int row, int pos, int k) {
+  return (uint32_t)row | (uint32_t)pos << 8 | (uint32_t)k << 16;
+}
 constexpr int LIST_BUCKETS = 8192;
 
 // Entries of each row tile sorted by vocabulary tile (in no order inside one: each has a place of its own to write to).
@@ -76,6 +82,168 @@ __global__ __launch_bounds__(1024) void distill_lists_kernel(const int64_t* __re
   if (n_vt % LIST_BUCKETS == 0 && tid == 0) list_begin[n_vt] = base;
 }
 
+// Merge of (m, a) pairs in units of 1 / T in slot order, as merge_fixed does it; NaN and +inf go through.
+template <int S>
+__device__ __forceinline__ void merge_scaled(const float (&m)[S], const float (&a)[S], float z_scale, float& M, float& A) {
+  M = NEG_INF;
+#pragma unroll
+  for (int k = 0; k < S; ++k) M = fmaxf(M, m[k]);
+  A = 0.f;
+#pragma unroll
+  for (int k = 0; k < S; ++k) if (a[k] != 0.f) A += a[k] * fast_exp2((m[k] - M) * z_scale);
+}
+
+template <typename T>
+struct DistillTileArgs {
+  const T* H; const T* HT; const T* W;
+  int N, d, V, n_rb, n_win, n_vt;
+  double vt_per_win;
+  float z_scale;                        // log2(e) / T
+  float* part; int64_t npad;            // [2][n_win][npad]: m, a per (window, row)
+  int item_begin;
+  // per row tile TILE * K entries, those of vocabulary tile q from list_begin[q] to list_begin[q + 1]
+  const int* list_begin; const uint32_t* entries; int K; float* zt;      // zt[row][place]
+};
+
+// The forward's tiles: its walk over a window's vocabulary tiles, its online (m, a) in units of 1 / T, and after each tile the logits
+// that the lists name there, 64 entries at a time with one entry per lane: a block of accumulators that holds one (ballot) is
+// read once more and the owning lane stores it.  Bound by the matrix instructions; the tests for entries are one comparison per
+// block of 16 logits per lane.  The logit handed out is the one in the row's sum bit for bit, which exp(z - lse) - share needs where
+// both are near 1 (a dot product of its own would also read N K rows of W, 2.1 GB at 8192 x 4096 with 32 entries a row).
+template <typename T, typename L, bool HKR>
+__global__ __launch_bounds__(L::THREADS, L::MIN_WAVES) void distill_tiles_kernel(DistillTileArgs<T> a) {
+  extern __shared__ __align__(16) char lds[];
+  constexpr int COLS = L::ROWS == 64 ? 16 : 32;         // token columns of a block
+  const int lane = threadIdx.x & 63;
+  const int id = a.item_begin + xcd_contiguous_id(blockIdx.x, gridDim.x);
+  int rb, win;
+  grouped_raster(id, a.n_rb, a.n_win, FLCE_FWD_GROUP, rb, win);
+  // (as the cross-entropy's forward places its windows)
+  const int vt_begin = __builtin_amdgcn_readfirstlane((int)(win * a.vt_per_win));
+  const int vt_end = win + 1 < a.n_win ? __builtin_amdgcn_readfirstlane((int)((win + 1) * a.vt_per_win)) : a.n_vt;
+  const int n0 = rb * L::TILE;
+  const int64_t ld_bytes = (int64_t)a.d * sizeof(T);
+  // The lists run two tiles ahead: a tile's range is loaded while the tile before the last is computed, its first entries while the
+  // last is, so that neither load is waited for ahead of a request.  A range is one vector register, its begin in even lanes
+  // and its end in odd ones: the loop has no scalar registers for it.
+  auto load_range = [&](int vt) { return a.list_begin[(int64_t)rb * (a.n_vt + 1) + vt + (lane & 1)]; };
+  auto load_entry = [&](int range, int first) {
+    const int at = __builtin_amdgcn_readlane(range, 0) + first + lane;
+    return at < __builtin_amdgcn_readlane(range, 1) ? a.entries[(int64_t)rb * (L::TILE * a.K) + at] : NO_ENTRY;
+  };
+  float m[L::WN], s[L::WN];
+#pragma unroll
+  for (int j = 0; j < L::WN; ++j) { m[j] = NEG_INF; s[j] = 0.f; }
+  int range = 0, range_next = 0;
+  uint32_t entry = NO_ENTRY;
+  typename L::Acc acc;
+  typename L::template Stream<HKR> stream;
+  if (vt_begin < vt_end) {
+    range = load_range(vt_begin);
+    range_next = load_range(min(vt_begin + 1, a.n_vt - 1));
+    entry = load_entry(range, 0);
+    asm volatile("" : "+v"(entry), "+v"(range_next));
+    stream.start(a.W, ld_bytes, vt_begin * L::TILE, a.V, a.H, a.HT, ld_bytes, n0, a.N, a.d, lds);
+  }
+  for (int vt = vt_begin; vt < vt_end; ++vt) {
+    const int v0 = vt * L::TILE;
+    uint32_t entry_next = NO_ENTRY;
+    int range2 = 0;
+    stream.run(lds, acc, [&] {
+      if (vt + 1 < vt_end) {
+        entry_next = load_entry(range_next, 0);
+        range2 = load_range(min(vt + 2, a.n_vt - 1));
+        stream.start(a.W, ld_bytes, v0 + L::TILE, a.V, a.H, a.HT, ld_bytes, n0, a.N, a.d, lds);
+      }
+    });
+#pragma unroll
+    for (int j = 0; j < L::WN; ++j) {
+#pragma unroll
+      for (int i = 0; i < L::WM; ++i) {
+        const int blk0 = v0 + __builtin_amdgcn_readfirstlane(L::tile_m(i, 0) & ~(L::ROWS - 1));   // first row of the block
+        if (blk0 >= a.V) continue;
+        float z[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) z[r] = acc.get(i, j, r);
+        if (blk0 + L::ROWS > a.V) {
+          const int live = a.V - blk0 - L::lane_row();
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if ((r >> 2) * L::QUAD + (r & 3) >= live) z[r] = NEG_INF;
+        }
+        float bmax = z[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) bmax = fmaxf(bmax, z[r]);
+        const float mn = fmaxf(m[j], bmax);
+        const float ms = (mn == NEG_INF) ? 0.f : mn;     // nothing but padding so far: keep exp arguments finite
+        const float msl = -ms * a.z_scale;
+        float sum = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum += fast_exp2(fmaf(z[r], a.z_scale, msl));
+        s[j] = s[j] * fast_exp2((m[j] - ms) * a.z_scale) + sum;
+        m[j] = mn;
+        __builtin_amdgcn_sched_barrier(0);     // one block at a time in VGPRs
+      }
+    }
+    const int count = __builtin_amdgcn_readlane(range, 1) - __builtin_amdgcn_readlane(range, 0);
+    for (int c = 0; c < count; c += 64) {
+      const uint32_t e = c == 0 ? entry : load_entry(range, c);
+      // the wavefront's block that holds the lane's entry, if one does (blocks are aligned to their size)
+      const int en = (int)(e & 255) - (L::tile_n(0) & ~(COLS - 1)), ev = (int)(e >> 8 & 255) - (L::tile_m(0, 0) & ~(L::ROWS - 1));
+      const bool mine = e != NO_ENTRY && en >= 0 && en < L::WN * COLS && ev >= 0 && ev < L::WM * L::ROWS;
+      const int block = mine ? en / COLS * L::WM + ev / L::ROWS : -1;
+#pragma unroll
+      for (int j = 0; j < L::WN; ++j) {
+#pragma unroll
+        for (int i = 0; i < L::WM; ++i) {
+          uint64_t hits = __ballot(block == j * L::WM + i);
+          if (hits != 0ull) {
+            float z[16];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) z[r] = acc.get(i, j, r);
+            do {
+              const int from = __builtin_ctzll(hits);
+              hits &= hits - 1;
+              const uint32_t h = __builtin_amdgcn_readlane(e, from);
+              // row rel of a block is register 4 (rel / QUAD) + rel % 4 of the lanes of quarter (or half) rel % QUAD / 4
+              const int rel = h >> 8 & (L::ROWS - 1), in = rel % L::QUAD, r = rel / L::QUAD * 4 + (in & 3);
+              float v = z[0];
+#pragma unroll
+              for (int k = 1; k < 16; ++k) v = r == k ? z[k] : v;
+              if (lane == in / 4 * COLS + (int)(h & (COLS - 1))) a.zt[(int64_t)(n0 + (int)(h & 255)) * a.K + (h >> 16)] = v;
+            } while (hits != 0ull);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+    asm volatile("" : "+v"(entry_next), "+v"(range2));
+    entry = entry_next; range = range_next; range_next = range2;
+  }
+
+  // SLOTS lanes hold partial state of each token: merged in fixed slot order through LDS (free after the main loop's last barrier)
+  constexpr int S = L::SLOTS;
+  float* sm = reinterpret_cast<float*>(lds);
+  float* sa = sm + S * L::TILE;
+  const int slot = L::slot();
+#pragma unroll
+  for (int j = 0; j < L::WN; ++j) {
+    sm[slot * L::TILE + L::tile_n(j)] = m[j];
+    sa[slot * L::TILE + L::tile_n(j)] = s[j];
+  }
+  __syncthreads();
+  if (threadIdx.x < L::TILE) {
+    float pm[S], pa[S];
+#pragma unroll
+    for (int k = 0; k < S; ++k) { pm[k] = sm[k * L::TILE + threadIdx.x]; pa[k] = sa[k * L::TILE + threadIdx.x]; }
+    float M, A;
+    merge_scaled<S>(pm, pa, a.z_scale, M, A);
+    const int64_t o = (int64_t)win * a.npad + n0 + threadIdx.x;
+    a.part[o] = M;
+    a.part[(int64_t)a.n_win * a.npad + o] = A;
+  }
+}
+
 // One row's list in the lanes of a wavefront: entry lane + 64 u is the lane's u-th.
 struct RowList {
   static constexpr int U = DISTILL_MAX / 64;
@@ -116,45 +284,42 @@ struct RowList {
   }
 };
 
-// The forward's end, a wavefront per row: lse from the groups' (max, sum), the row's loss; per-block sums in fixed order, and
-// the call's loss from them by the block that hands its sums in last (merge_rows_kernel's way).  Bound by the read of the groups' pairs.
+// The forward's end, a wavefront per row: lse from the windows' (m, a), the row's loss; per-block sums in fixed order, and
+// the call's loss from them by the block that hands its sums in last (merge_rows_kernel's way).  A chain of latencies.
 constexpr int DISTILL_ROWS = 4;
 struct DistillRowArgs {
   const int64_t* ids; const float* t; const float* zt;
-  int row0, rows, V, K, n_groups;
-  const float2* stats; int64_t ld_stats;
+  int N, V, K, n_win;
+  const float* part; int64_t npad;
   float temperature, inv_T, z_scale;
   float* lse_out; float* loss_rows_out;
-  LossOut o; int blk0, n_blk;             // this launch's first block among all of the call's
+  LossOut o;
 };
 static __global__ __launch_bounds__(64 * DISTILL_ROWS) void distill_rows_kernel(DistillRowArgs a) {
   __shared__ float sl[DISTILL_ROWS];
   __shared__ int sc[DISTILL_ROWS], so[DISTILL_ROWS], last;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int r = blockIdx.x * DISTILL_ROWS + wave;
+  const int64_t n = (int64_t)blockIdx.x * DISTILL_ROWS + wave;
   float loss = 0.f;
   bool counts = false, oor = false;
-  if (r < a.rows) {
-    const int64_t n = a.row0 + r;
-    const float2* __restrict__ s = a.stats + (int64_t)r * a.ld_stats;
+  if (n < a.N) {
+    const float* __restrict__ pm = a.part + n;
+    const float* __restrict__ pa = pm + (int64_t)a.n_win * a.npad;
+    float m = NEG_INF, sum = 0.f;
     RowList list;
     list.load(a.ids + n * a.K, a.t + n * a.K, a.K, a.V, a.inv_T);
     float z[RowList::U];
 #pragma unroll
     for (int u = 0; u < RowList::U; ++u) z[u] = list.id[u] >= 0 ? a.zt[n * a.K + lane + 64 * u] : 0.f;
-    float m = NEG_INF;
-#pragma unroll 8
-    for (int g = lane; g < a.n_groups; g += 64) m = fmaxf(m, s[g].x);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-    m = finite_or_zero(m);
-    float sum = 0.f;
-#pragma unroll 8
-    for (int g = lane; g < a.n_groups; g += 64) {
-      const float2 x = s[g];
-      if (x.y != 0.f) sum += x.y * fast_exp2((finite_or_zero(x.x) - m) * a.z_scale);
+    for (int w = lane; w < a.n_win; w += 64) {
+      const float mw[2] = {m, pm[w * a.npad]}, aw[2] = {sum, pa[w * a.npad]};
+      merge_scaled<2>(mw, aw, a.z_scale, m, sum);
     }
-    sum = wave_sum(sum);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      const float mw[2] = {m, __shfl_xor(m, o, 64)}, aw[2] = {sum, __shfl_xor(sum, o, 64)};
+      merge_scaled<2>(mw, aw, a.z_scale, m, sum);
+    }
     const float lse = fmaf(m, a.inv_T, logf(sum));
     counts = list.counts;
     oor = list.out_of_range;
@@ -176,15 +341,15 @@ static __global__ __launch_bounds__(64 * DISTILL_ROWS) void distill_rows_kernel(
     int c = 0, bad = 0;
 #pragma unroll
     for (int w = 0; w < DISTILL_ROWS; ++w) { l += sl[w]; c += sc[w]; bad |= so[w]; }
-    const int b = a.blk0 + blockIdx.x;
+    const int b = blockIdx.x;
     __hip_atomic_store(a.o.blk_loss + b, l, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __hip_atomic_store(a.o.blk_cnt + b, c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __hip_atomic_store(a.o.blk_oor + b, bad, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // the three stores have reached the point the other XCDs read from
-    last = __hip_atomic_fetch_add(&a.o.hdr->arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)a.n_blk - 1;
+    last = __hip_atomic_fetch_add(&a.o.hdr->arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
   }
   __syncthreads();
-  if (last) finalize_loss(a.o, a.n_blk);
+  if (last) finalize_loss(a.o, gridDim.x);
 }
 
 // The backward's start, a wavefront per row: shares (the whole share of an id at its first place in the row, -1 at the others and

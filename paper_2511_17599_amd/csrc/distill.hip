@@ -42,14 +42,10 @@ FLCE_DISTILL(float, F32Loop<128>)
 
 namespace {
 
-// The groups' pairs of a chunk of rows wait in memory for their sum.
-constexpr int64_t DISTILL_STATS_BYTES = (int64_t)256 << 20;
-
 struct DistillPlan {
   Plan p;
-  int tile, group, n_groups, n_blk;
-  int64_t ld_stats, rows;
-  int64_t off_blk_loss, off_blk_cnt, off_blk_oor, off_stats, off_begin, off_entries, off_HT, fwd_bytes;
+  int tile, n_blk;
+  int64_t off_blk_loss, off_blk_cnt, off_blk_oor, off_part, off_begin, off_entries, off_HT, fwd_bytes;
   int64_t off_share, off_target, off_grad, off_grad_rows, bwd_bytes;
 };
 
@@ -58,19 +54,13 @@ bool make_distill_plan(int parts, int64_t N, int64_t d, int64_t V, int64_t K, fl
   const Plan& p = x.p;
   if (parts & PLAN_FORWARD) {
     x.tile = p.esize == 2 && !p.fast ? TILE : p.fwd_tile;
-    x.group = p.fast ? 64 : 32;
-    x.n_groups = (int)ceil_div(V, x.group);
-    x.ld_stats = align_up(V, TILE) / x.group;
-    const int64_t most = std::max<int64_t>(TILE, DISTILL_STATS_BYTES / (x.ld_stats * 8) / TILE * TILE);
-    x.rows = align_up(ceil_div(p.npad, ceil_div(p.npad, most)), TILE);
-    x.n_blk = 0;
-    for (int64_t r = 0; r < N; r += x.rows) x.n_blk += (int)ceil_div(std::min(x.rows, N - r), DISTILL_ROWS);
+    x.n_blk = (int)ceil_div(N, DISTILL_ROWS);
     const int64_t n_rt = ceil_div(N, x.tile), n_vt = ceil_div(V, x.tile);
     int64_t o = ALIGN;
     x.off_blk_loss = o; o = align_up(o + (int64_t)x.n_blk * 4, ALIGN);
     x.off_blk_cnt = o;  o = align_up(o + (int64_t)x.n_blk * 4, ALIGN);
     x.off_blk_oor = o;  o = align_up(o + (int64_t)x.n_blk * 4, ALIGN);
-    x.off_stats = o;    o = align_up(o + x.rows * x.ld_stats * 8, ALIGN);
+    x.off_part = o;     o = align_up(o + 2ll * p.n_win * p.npad * 4, ALIGN);
     x.off_begin = o;    o = align_up(o + n_rt * (n_vt + 1) * 4, ALIGN);
     x.off_entries = o;  o = align_up(o + n_rt * x.tile * K * 4, ALIGN);
     x.off_HT = o;       if (p.fwd_copy) o = align_up(o + packed_block_offset(p.n_rb, (int)d), ALIGN);
@@ -85,6 +75,18 @@ bool make_distill_plan(int parts, int64_t N, int64_t d, int64_t V, int64_t K, fl
     x.bwd_bytes = o;
   }
   return true;
+}
+
+template <typename T, typename L>
+hipError_t distill_tiles_allowance() {
+  static OncePerDevice once;
+  return once([] {
+    if constexpr (L::TUNED) {
+      const hipError_t e = allow_big_lds(distill_tiles_kernel<T, L, true>, L::LDS);
+      if (e != hipSuccess) return e;
+    }
+    return allow_big_lds(distill_tiles_kernel<T, L, false>, L::LDS);
+  });
 }
 
 bool temperature_ok(float T) { return T > 0.f && std::isfinite(T) && std::isfinite(LOG2E / T) && std::isfinite(T * T) && T * T > 0.f; }
@@ -120,7 +122,7 @@ flce_status flce_distill_forward(const void* H, const void* W, const int64_t* te
   char* ws = static_cast<char*>(workspace);
   const Plan& p = x.p;
   Header* hdr = reinterpret_cast<Header*>(ws);
-  float2* stats = reinterpret_cast<float2*>(ws + x.off_stats);
+  float* part = reinterpret_cast<float*>(ws + x.off_part);
   int* begin = reinterpret_cast<int*>(ws + x.off_begin);
   uint32_t* entries = reinterpret_cast<uint32_t*>(ws + x.off_entries);
   void* HT = p.fwd_copy ? ws + x.off_HT : nullptr;
@@ -128,39 +130,37 @@ flce_status flce_distill_forward(const void* H, const void* W, const int64_t* te
   return with_forward_loop(p, [&](auto tag) -> flce_status {
     using T = typename decltype(tag)::T;
     using L = typename decltype(tag)::L;
-    if (logit_tiles_allowance<T, L, false>() != hipSuccess) return FLCE_ERR_HIP;
-    const int n_vt = (int)ceil_div(V, L::TILE);
+    if (distill_tiles_allowance<T, L>() != hipSuccess) return FLCE_ERR_HIP;
+    const int n_rb = (int)ceil_div(N, L::TILE), n_vt = (int)ceil_div(V, L::TILE), items = n_rb * p.n_win;
     {
       ProfScope ps(FLCE_PROF_FWD_EPILOGUE, st);
-      distill_lists_kernel<L::TILE><<<(unsigned)ceil_div(N, L::TILE), 1024, 0, st>>>(teacher_ids, teacher_logits, (int)N, (int)V, (int)K, n_vt,
-                                                                                     begin, entries, zt_out, hdr);
+      distill_lists_kernel<L::TILE><<<(unsigned)n_rb, 1024, 0, st>>>(teacher_ids, teacher_logits, (int)N, (int)V, (int)K, n_vt, begin, entries,
+                                                                     zt_out, hdr);
     }
-    int blk0 = 0;
-    for (int64_t row0 = 0; row0 < N; row0 += x.rows) {
-      const int64_t rows = std::min<int64_t>(x.rows, N - row0);
-      LogitArgs<T> a{};
-      a.H = static_cast<const T*>(H); a.HT = static_cast<const T*>(HT); a.W = static_cast<const T*>(W);
-      a.N = (int)N; a.d = (int)d; a.V = (int)V;
-      a.nt0 = (int)(row0 / L::TILE); a.n_nt = (int)ceil_div(rows, L::TILE); a.n_vt = n_vt;
-      a.z_scale = LOG2E / temperature;
-      a.stats = stats; a.ld_stats = x.ld_stats;
-      a.list_begin = begin; a.entries = entries; a.K = (int)K; a.zt = zt_out;
-      {
-        ProfScope ps(FLCE_PROF_FWD_TILES, st);
-        launch_logit_tiles<T, L, false>(a, st);
+    {
+      // one workgroup per (row block, window), with the tuned loop a round of them per launch, as the cross-entropy's forward
+      ProfScope ps(FLCE_PROF_FWD_TILES, st);
+      int per_launch = items;
+      if constexpr (L::TUNED) per_launch = NUM_CU * L::PER_CU;
+      for (int item0 = 0; item0 < items; item0 += per_launch) {
+        const DistillTileArgs<T> a{static_cast<const T*>(H), static_cast<const T*>(HT), static_cast<const T*>(W), (int)N, (int)d, (int)V, n_rb,
+                                   p.n_win, n_vt, (double)n_vt / p.n_win, LOG2E / temperature, part, p.npad, item0, begin, entries, (int)K,
+                                   zt_out};
+        const int grid = std::min(per_launch, items - item0);
+        if constexpr (L::TUNED) {
+          if (HT) { distill_tiles_kernel<T, L, true><<<grid, L::THREADS, L::LDS, st>>>(a); continue; }
+        }
+        distill_tiles_kernel<T, L, false><<<grid, L::THREADS, L::LDS, st>>>(a);
       }
-      ProfScope ps(FLCE_PROF_FWD_EPILOGUE, st);
-      const int n_blk = (int)ceil_div(rows, DISTILL_ROWS);
-      // a call for rows alone has no scalar loss to hand out: the sum goes to a spare word of the header block
-      float* scalar = loss_out ? loss_out : reinterpret_cast<float*>(ws + 64);
-      distill_rows_kernel<<<n_blk, 64 * DISTILL_ROWS, 0, st>>>(DistillRowArgs{
-          teacher_ids, teacher_logits, zt_out, (int)row0, (int)rows, (int)V, (int)K, x.n_groups, stats, x.ld_stats, temperature,
-          1.f / temperature, LOG2E / temperature, lse_out, loss_rows_out,
-          LossOut{reinterpret_cast<float*>(ws + x.off_blk_loss), reinterpret_cast<int*>(ws + x.off_blk_cnt),
-                  reinterpret_cast<int*>(ws + x.off_blk_oor), hdr, scalar, reduction == FLCE_REDUCE_MEAN, nullptr, nullptr},
-          blk0, x.n_blk});
-      blk0 += n_blk;
     }
+    ProfScope ps(FLCE_PROF_FWD_EPILOGUE, st);
+    // a call for rows alone has no scalar loss to hand out: the sum goes to a spare word of the header block
+    float* scalar = loss_out ? loss_out : reinterpret_cast<float*>(ws + 64);
+    distill_rows_kernel<<<x.n_blk, 64 * DISTILL_ROWS, 0, st>>>(DistillRowArgs{
+        teacher_ids, teacher_logits, zt_out, (int)N, (int)V, (int)K, p.n_win, part, p.npad, temperature, 1.f / temperature,
+        LOG2E / temperature, lse_out, loss_rows_out,
+        LossOut{reinterpret_cast<float*>(ws + x.off_blk_loss), reinterpret_cast<int*>(ws + x.off_blk_cnt),
+                reinterpret_cast<int*>(ws + x.off_blk_oor), hdr, scalar, reduction == FLCE_REDUCE_MEAN, nullptr, nullptr}});
     return hipGetLastError() == hipSuccess ? FLCE_OK : FLCE_ERR_HIP;
   });
 }

@@ -81,19 +81,18 @@ flce_status run_topk(const TopkPlan& t, const void* H, const void* W, int K, cha
   return with_forward_loop(p, [&](auto tag) -> flce_status {
     using T = typename decltype(tag)::T;
     using L = typename decltype(tag)::L;
-    if (logit_tiles_allowance<T, L, true>() != hipSuccess) return FLCE_ERR_HIP;
+    if (logit_tiles_allowance<T, L>() != hipSuccess) return FLCE_ERR_HIP;
     for (int64_t row0 = 0; row0 < N; row0 += t.rows) {
       const int64_t rows = std::min<int64_t>(t.rows, N - row0);
       LogitArgs<T> a{};
       a.H = static_cast<const T*>(H); a.HT = static_cast<const T*>(HT); a.W = static_cast<const T*>(W);
       a.N = N; a.d = d; a.V = V;
       a.nt0 = (int)(row0 / L::TILE); a.n_nt = (int)ceil_div(rows, L::TILE); a.n_vt = (int)ceil_div(V, L::TILE);
-      a.z_scale = LOG2E;
       a.stats = stats; a.ld_stats = t.ld_stats;
       a.z = z; a.ldz = t.ldz;
       {
         ProfScope ps(FLCE_PROF_FWD_TILES, st);
-        launch_logit_tiles<T, L, true>(a, st);
+        launch_logit_tiles<T, L>(a, st);
       }
       ProfScope ps(FLCE_PROF_FWD_EPILOGUE, st);
       launch_select(t, rows, row0, K, ws, logits, ids, lse, st);
