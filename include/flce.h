@@ -343,23 +343,24 @@ flce_status flce_topk(const void* H, const void* W, int64_t N, int64_t d, int64_
  *   K             : 1 .. 256.   temperature : positive and finite, as are T^2 and 1 / T.
  *   loss_out      : device, 1 float, the mean over the rows that count or the sum; may be NULL if loss_rows_out is not.
  *   loss_rows_out : device, N floats; may be NULL if loss_out is not.
- *   lse_out       : device, N floats, of the logits / T, for every row.    zt_out : device, N*K floats, the student's logits at the
- *                   list's ids (0 where there is no share); the backward takes both back.
+ *   lse_out       : device, N floats, of the logits / T, for every row.
+ *   saved_out     : device, flce_distill_saved_bytes(N, K) bytes, 16-byte aligned: shares and the student's logits at the lists' ids.  The
+ *                   backward takes lse and saved back, with the same ids, K and T.
  *   grad_loss     : device, 1 float, the upstream gradient of the scalar loss, or NULL;
  *   grad_rows     : device, N floats, of the losses per row (sum semantics), or NULL: exactly one of the two.
  * G = dloss/dZ is rounded to `dt` before the two contractions, as flce_backward's and flce_backward_rows' is.
  * Workspaces: flce_distill_workspace_bytes(N, d, V, K, dt, for_backward) bytes, 0 for an invalid shape.  Forward: 8 bytes per window
  * and row, the lists by tile (4 bytes per entry, and per pair of a row and a vocabulary tile), flce_forward's copy of H; backward:
- * flce_backward's and 4 bytes per list entry.
+ * flce_backward's.
  */
 size_t flce_distill_workspace_bytes(int64_t N, int64_t d, int64_t V, int64_t K, flce_dtype dt, int for_backward);
+size_t flce_distill_saved_bytes(int64_t N, int64_t K);
 flce_status flce_distill_forward(const void* H, const void* W, const int64_t* teacher_ids, const float* teacher_logits,
                                  int64_t N, int64_t d, int64_t V, int64_t K, float temperature,
                                  flce_reduction reduction, flce_dtype dt,
-                                 float* loss_out, float* loss_rows_out, float* lse_out, float* zt_out,
+                                 float* loss_out, float* loss_rows_out, float* lse_out, void* saved_out,
                                  void* workspace, size_t workspace_bytes, void* hip_stream);
-flce_status flce_distill_backward(const void* H, const void* W, const int64_t* teacher_ids, const float* teacher_logits,
-                                  const float* lse, const float* zt,
+flce_status flce_distill_backward(const void* H, const void* W, const int64_t* teacher_ids, const float* lse, const void* saved,
                                   int64_t N, int64_t d, int64_t V, int64_t K, float temperature,
                                   flce_reduction reduction, flce_dtype dt, const float* grad_loss, const float* grad_rows,
                                   void* dH_out, void* dW_out,

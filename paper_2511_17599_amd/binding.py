@@ -23,6 +23,7 @@ EXPORTS = ("flce_version", "flce_tuning_reload", "flce_status_string", "flce_wor
            "flce_forward_with_grads", "flce_scale", "flce_forward_rows", "flce_backward_rows", "flce_forward_partial", "flce_merge_workspace_bytes",
            "flce_merge_partials", "flce_backward_partial", "flce_last_device_status", "flce_profile_enable",
            "flce_profile_collect", "flce_probe", "flce_topk_workspace_bytes", "flce_topk", "flce_distill_workspace_bytes",
+           "flce_distill_saved_bytes",
            "flce_distill_forward", "flce_distill_backward", "flce_beam_workspace_bytes", "flce_beam_step", "flce_beam_reorder")
 PROF_CLASSES = ("fwd_tiles", "fwd_epilogue", "bwd_prep", "recompute", "contract_dW", "contract_dH", "scale")
 
@@ -106,7 +107,8 @@ def lib():
                 ("flce_topk", i, [p, p, i64, i64, i64, i64, i, p, p, p, p, sz, p]),
                 ("flce_distill_workspace_bytes", sz, [i64, i64, i64, i64, i, i]),
                 ("flce_distill_forward", i, [p, p, p, p, i64, i64, i64, i64, f, i, i, p, p, p, p, p, sz, p]),
-                ("flce_distill_backward", i, [p, p, p, p, p, p, i64, i64, i64, i64, f, i, i, p, p, p, p, p, sz, p]),
+                ("flce_distill_saved_bytes", sz, [i64, i64]),
+                ("flce_distill_backward", i, [p, p, p, p, p, i64, i64, i64, i64, f, i, i, p, p, p, p, p, sz, p]),
                 ("flce_beam_workspace_bytes", sz, [i64, i64, i64, i64, i64, i]),
                 ("flce_beam_step", i, [p, p, p, p, i64, i64, i64, i64, i64, i64, i64, i, p, p, p, p, p, sz, p]),
                 ("flce_beam_reorder", i, [p, p, p, i64, i64, i64, i64, i64, i64, i64, i64, i64, p, p])):
@@ -247,17 +249,21 @@ def flce_distill_workspace_bytes(N, d, V, K, dt, for_backward):
     return int(lib().flce_distill_workspace_bytes(N, d, V, K, dt, int(bool(for_backward))))
 
 
+def flce_distill_saved_bytes(N, K):
+    return int(lib().flce_distill_saved_bytes(N, K))
+
+
 def flce_distill_forward(H, W, teacher_ids, teacher_logits, N, d, V, K, temperature, reduction, dt, loss_out, loss_rows_out,
-                         lse_out, zt_out, workspace, workspace_bytes, hip_stream=None):
+                         lse_out, saved_out, workspace, workspace_bytes, hip_stream=None):
     return lib().flce_distill_forward(_ptr(H), _ptr(W), _ptr(teacher_ids), _ptr(teacher_logits), N, d, V, K,
                                       float(temperature), reduction, dt, _ptr(loss_out), _ptr(loss_rows_out), _ptr(lse_out),
-                                      _ptr(zt_out), _ptr(workspace), workspace_bytes, _stream(hip_stream))
+                                      _ptr(saved_out), _ptr(workspace), workspace_bytes, _stream(hip_stream))
 
 
-def flce_distill_backward(H, W, teacher_ids, teacher_logits, lse, zt, N, d, V, K, temperature, reduction, dt, grad_loss,
-                          grad_rows, dH_out, dW_out, workspace, workspace_bytes, hip_stream=None):
-    return lib().flce_distill_backward(_ptr(H), _ptr(W), _ptr(teacher_ids), _ptr(teacher_logits), _ptr(lse), _ptr(zt), N, d, V,
-                                       K, float(temperature), reduction, dt, _ptr(grad_loss), _ptr(grad_rows), _ptr(dH_out),
+def flce_distill_backward(H, W, teacher_ids, lse, saved, N, d, V, K, temperature, reduction, dt, grad_loss, grad_rows, dH_out,
+                          dW_out, workspace, workspace_bytes, hip_stream=None):
+    return lib().flce_distill_backward(_ptr(H), _ptr(W), _ptr(teacher_ids), _ptr(lse), _ptr(saved), N, d, V, K,
+                                       float(temperature), reduction, dt, _ptr(grad_loss), _ptr(grad_rows), _ptr(dH_out),
                                        _ptr(dW_out), _ptr(workspace), workspace_bytes, _stream(hip_stream))
 
 

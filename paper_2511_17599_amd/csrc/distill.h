@@ -1,4 +1,4 @@
-// Distillation from a teacher's largest logits: the lists by tile for the forward's tiles, a row's loss, the shares the backward
+// Distillation from a teacher's largest logits: the lists by tile, the forward's tiles, a row's loss and the shares that the backward
 // subtracts, and their place in G.
 //   p_k = softmax over the list of t_k / T;  loss = T^2 sum_k p_k (log p_k - z_{id_k} / T + lse),  lse = log sum_v exp(z_v / T)
 //   d loss / d z_v = T (exp(z_v / T - lse) - sum of p_k with id_k = v)
@@ -18,34 +18,54 @@ __host__ __device__ __forceinline__ constexpr uint32_t list_entry(int row, int p
 constexpr int LIST_BUCKETS = 8192;
 
 // Entries of each row tile sorted by vocabulary tile (in no order inside one: each has a place of its own to write to).
-// One block per row tile: count, prefix sum, place; a chain of latencies, two reads of the lists.
+// One block per row tile: count, prefix sum, place.  A chain of latencies: a thread's first LIST_HELD entries are loaded together and
+// stay in registers (256 rows x 32 entries are all of them; 2048 rows 18.4 -> LISTS_US us), further ones are read twice.
+constexpr int LIST_HELD = 8;
 template <int E>
 __global__ __launch_bounds__(1024) void distill_lists_kernel(const int64_t* __restrict__ ids, const float* __restrict__ t, int N, int V, int K,
                                                              int n_vt, int* __restrict__ list_begin, uint32_t* __restrict__ entries,
-                                                             float* __restrict__ zt, Header* __restrict__ hdr) {
+                                                             float2* __restrict__ saved, Header* __restrict__ hdr) {
   __shared__ int cnt[LIST_BUCKETS];
   __shared__ int wsum[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int n0 = blockIdx.x * E, total = min(E, N - n0) * K;
-  ids += (int64_t)n0 * K; t += (int64_t)n0 * K; zt += (int64_t)n0 * K;
+  ids += (int64_t)n0 * K; t += (int64_t)n0 * K; saved += (int64_t)n0 * K;
   list_begin += (int64_t)blockIdx.x * (n_vt + 1);
   entries += (int64_t)blockIdx.x * E * K;
   if (blockIdx.x == 0 && tid == 0) hdr->arrived = 0;      // for the loss that follows on the stream
-  auto listed = [&](int i, int64_t& id) {
-    id = ids[i];
-    return id >= 0 && id < V && t[i] != NEG_INF;
+  // id of entry i, -1 where it has no share
+  auto share_id = [&](int64_t id, float x) { return id >= 0 && id < V && x != NEG_INF ? (int)id : -1; };
+  int held[LIST_HELD];
+  {
+    int64_t id[LIST_HELD];
+    float x[LIST_HELD];
+#pragma unroll
+    for (int u = 0; u < LIST_HELD; ++u) {
+      const int i = min(tid + u * 1024, total - 1);
+      id[u] = ids[i]; x[u] = t[i];
+    }
+#pragma unroll
+    for (int u = 0; u < LIST_HELD; ++u) held[u] = tid + u * 1024 < total ? share_id(id[u], x[u]) : -1;
+  }
+  // f(i, id) for every entry with a share
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int u = 0; u < LIST_HELD; ++u)
+      if (held[u] >= 0) f(tid + u * 1024, held[u]);
+    for (int i = tid + LIST_HELD * 1024; i < total; i += 1024) {
+      const int id = share_id(ids[i], t[i]);
+      if (id >= 0) f(i, id);
+    }
   };
   int base = 0;
   for (int q0 = 0; q0 < n_vt; q0 += LIST_BUCKETS) {
+    const int nq = min(LIST_BUCKETS, n_vt + 1 - q0);        // (with the one behind the last tile: the end)
     for (int i = tid; i < LIST_BUCKETS; i += 1024) cnt[i] = 0;
     __syncthreads();
-    for (int i = tid; i < total; i += 1024) {
-      int64_t id;
-      const bool in = listed(i, id);
-      if (q0 == 0 && !in) zt[i] = 0.f;
-      const int q = in ? (int)id / E - q0 : -1;
+    each([&](int, int id) {
+      const int q = id / E - q0;
       if (q >= 0 && q < LIST_BUCKETS) atomicAdd(&cnt[q], 1);
-    }
+    });
     __syncthreads();
     constexpr int PER = LIST_BUCKETS / 1024;
     int own[PER], sum = 0;
@@ -63,19 +83,14 @@ __global__ __launch_bounds__(1024) void distill_lists_kernel(const int64_t* __re
 #pragma unroll
     for (int w = 0; w < 16; ++w) { if (w < wave) at += wsum[w]; all += wsum[w]; }
 #pragma unroll
-    for (int k = 0; k < PER; ++k) {
-      const int q = tid * PER + k;
-      cnt[q] = at;
-      if (q0 + q <= n_vt) list_begin[q0 + q] = at;        // (the one behind the last tile: the end)
-      at += own[k];
-    }
+    for (int k = 0; k < PER; ++k) { cnt[tid * PER + k] = at; at += own[k]; }
     __syncthreads();
-    for (int i = tid; i < total; i += 1024) {
-      int64_t id;
-      if (!listed(i, id)) continue;
-      const int q = (int)id / E - q0;
-      if (q >= 0 && q < LIST_BUCKETS) entries[atomicAdd(&cnt[q], 1)] = list_entry(i / K, (int)id % E, i % K);
-    }
+    for (int i = tid; i < nq; i += 1024) list_begin[q0 + i] = cnt[i];
+    __syncthreads();
+    each([&](int i, int id) {
+      const int q = id / E - q0;
+      if (q >= 0 && q < LIST_BUCKETS) entries[atomicAdd(&cnt[q], 1)] = list_entry(i / K, id % E, i % K);
+    });
     base += all;
     __syncthreads();
   }
@@ -102,7 +117,7 @@ struct DistillTileArgs {
   float* part; int64_t npad;            // [2][n_win][npad]: m, a per (window, row)
   int item_begin;
   // per row tile TILE * K entries, those of vocabulary tile q from list_begin[q] to list_begin[q + 1]
-  const int* list_begin; const uint32_t* entries; int K; float* zt;      // zt[row][place]
+  const int* list_begin; const uint32_t* entries; int K; float2* saved;  // saved[row][place].y: the logit
 };
 
 // The forward's tiles: its walk over a window's vocabulary tiles, its online (m, a) in units of 1 / T, and after each tile the logits
@@ -210,7 +225,7 @@ __global__ __launch_bounds__(L::THREADS, L::MIN_WAVES) void distill_tiles_kernel
               float v = z[0];
 #pragma unroll
               for (int k = 1; k < 16; ++k) v = r == k ? z[k] : v;
-              if (lane == in / 4 * COLS + (int)(h & (COLS - 1))) a.zt[(int64_t)(n0 + (int)(h & 255)) * a.K + (h >> 16)] = v;
+              if (lane == in / 4 * COLS + (int)(h & (COLS - 1))) a.saved[(int64_t)(n0 + (int)(h & 255)) * a.K + (h >> 16)].y = v;
             } while (hits != 0ull);
           }
           __builtin_amdgcn_sched_barrier(0);
@@ -284,11 +299,13 @@ struct RowList {
   }
 };
 
-// The forward's end, a wavefront per row: lse from the windows' (m, a), the row's loss; per-block sums in fixed order, and
-// the call's loss from them by the block that hands its sums in last (merge_rows_kernel's way).  A chain of latencies.
+// The forward's end, a wavefront per row: lse from the windows' (m, a), the row's loss, and what the backward needs: shares (the
+// whole share of an id at its first place in the row, -1 at the others and where there is none) and the target that the row preparation
+// counts rows by (V: counts, matches no column; -1: does not count; V + 1: out of range).  Per-block sums in fixed order, and the
+// call's loss from them by the block that hands its sums in last (merge_rows_kernel's way).  A chain of latencies.
 constexpr int DISTILL_ROWS = 4;
 struct DistillRowArgs {
-  const int64_t* ids; const float* t; const float* zt;
+  const int64_t* ids; const float* t; float2* saved; int64_t* target;
   int N, V, K, n_win;
   const float* part; int64_t npad;
   float temperature, inv_T, z_scale;
@@ -296,6 +313,8 @@ struct DistillRowArgs {
   LossOut o;
 };
 static __global__ __launch_bounds__(64 * DISTILL_ROWS) void distill_rows_kernel(DistillRowArgs a) {
+  __shared__ int sid[DISTILL_ROWS][DISTILL_MAX];
+  __shared__ float sp[DISTILL_ROWS][DISTILL_MAX];
   __shared__ float sl[DISTILL_ROWS];
   __shared__ int sc[DISTILL_ROWS], so[DISTILL_ROWS], last;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -307,10 +326,13 @@ static __global__ __launch_bounds__(64 * DISTILL_ROWS) void distill_rows_kernel(
     const float* __restrict__ pa = pm + (int64_t)a.n_win * a.npad;
     float m = NEG_INF, sum = 0.f;
     RowList list;
-    list.load(a.ids + n * a.K, a.t + n * a.K, a.K, a.V, a.inv_T);
+    float2* __restrict__ saved = a.saved + n * a.K;
     float z[RowList::U];
 #pragma unroll
-    for (int u = 0; u < RowList::U; ++u) z[u] = list.id[u] >= 0 ? a.zt[n * a.K + lane + 64 * u] : 0.f;
+    for (int u = 0; u < RowList::U; ++u) z[u] = lane + 64 * u < a.K ? saved[lane + 64 * u].y : 0.f;      // (undefined without a share)
+    list.load(a.ids + n * a.K, a.t + n * a.K, a.K, a.V, a.inv_T);
+#pragma unroll
+    for (int u = 0; u < RowList::U; ++u) { sid[wave][lane + 64 * u] = list.id[u]; sp[wave][lane + 64 * u] = list.p[u]; }
     for (int w = lane; w < a.n_win; w += 64) {
       const float mw[2] = {m, pm[w * a.npad]}, aw[2] = {sum, pa[w * a.npad]};
       merge_scaled<2>(mw, aw, a.z_scale, m, sum);
@@ -329,8 +351,22 @@ static __global__ __launch_bounds__(64 * DISTILL_ROWS) void distill_rows_kernel(
       if (list.id[u] >= 0 && list.p[u] != 0.f) kl += list.p[u] * ((list.x[u] - list.log_sum) + fmaf(-z[u], a.inv_T, lse));
     kl = wave_sum(kl);
     loss = counts ? a.temperature * a.temperature * kl : 0.f;
+#pragma unroll
+    for (int u = 0; u < RowList::U; ++u) {
+      if (64 * u >= a.K) break;
+      const int k = lane + 64 * u;
+      float share = 0.f;
+      bool first = list.id[u] >= 0;
+      for (int o = 0; o < a.K; ++o) {          // (a wavefront reads what it wrote: LDS operations of one are in order)
+        const bool same = sid[wave][o] == list.id[u];
+        if (same) share += sp[wave][o];
+        first = first && !(same && o < k);
+      }
+      if (k < a.K) saved[k] = float2{first ? share : -1.f, list.id[u] >= 0 ? z[u] : 0.f};
+    }
     if (lane == 0) {
       a.lse_out[n] = lse;
+      a.target[n] = oor ? (int64_t)a.V + 1 : counts ? a.V : -1;
       if (a.loss_rows_out) a.loss_rows_out[n] = loss;
     }
   }
@@ -352,48 +388,6 @@ static __global__ __launch_bounds__(64 * DISTILL_ROWS) void distill_rows_kernel(
   if (last) finalize_loss(a.o, gridDim.x);
 }
 
-// The backward's start, a wavefront per row: shares (the whole share of an id at its first place in the row, -1 at the others and
-// where there is none), the targets that the row preparation counts rows by (V: counts, matches no column; -1: does not count;
-// V + 1: out of range), upstream gradients times T.
-struct DistillPrepArgs {
-  const int64_t* ids; const float* t; int N, V, K; float inv_T, temperature;
-  float* share; int64_t* target;
-  const float* grad_loss; const float* grad_rows; float* grad_loss_T; float* grad_rows_T;
-};
-static __global__ __launch_bounds__(64 * DISTILL_ROWS) void distill_prep_kernel(DistillPrepArgs a) {
-  __shared__ int sid[DISTILL_ROWS][DISTILL_MAX];
-  __shared__ float sp[DISTILL_ROWS][DISTILL_MAX];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t n = (int64_t)blockIdx.x * DISTILL_ROWS + wave;
-  if (n == 0 && lane == 0 && a.grad_loss) *a.grad_loss_T = *a.grad_loss * a.temperature;
-  const bool row = n < a.N;
-  RowList list;
-  if (row) {
-    list.load(a.ids + n * a.K, a.t + n * a.K, a.K, a.V, a.inv_T);
-#pragma unroll
-    for (int u = 0; u < RowList::U; ++u) { sid[wave][lane + 64 * u] = list.id[u]; sp[wave][lane + 64 * u] = list.p[u]; }
-  }
-  __syncthreads();
-  if (!row) return;
-  if (lane == 0) {
-    a.target[n] = list.out_of_range ? (int64_t)a.V + 1 : list.counts ? a.V : -1;
-    if (a.grad_rows) a.grad_rows_T[n] = a.grad_rows[n] * a.temperature;
-  }
-#pragma unroll
-  for (int u = 0; u < RowList::U; ++u) {
-    const int k = lane + 64 * u;
-    if (64 * u >= a.K) break;
-    float sum = 0.f;
-    bool first = list.id[u] >= 0;
-    for (int o = 0; o < a.K; ++o) {
-      const bool same = sid[wave][o] == list.id[u];
-      if (same) sum += sp[wave][o];
-      first = first && !(same && o < k);
-    }
-    if (k < a.K) a.share[n * a.K + k] = first ? sum : -1.f;
-  }
-}
-
 // The listed elements of a staged chunk of G: exp(z / T - lse) - share, from the forward's logit and in one rounding, over what the
 // recompute step wrote there (which knows no lists).  A thread per entry of the chunk's rows.
 template <typename T, typename L, bool PER_ROW>
@@ -403,12 +397,12 @@ __global__ __launch_bounds__(256) void distill_scatter_kernel(RecomputeArgs<T> a
   const int c = a.nt0 * L::TILE + rl;
   if (rl >= a.n_nt * L::TILE || c >= a.hdr->n_valid) return;
   const int64_t at = (int64_t)rowmap[c] * x.K + k;
-  const float share = x.share[at];
-  if (share < 0.f) return;
+  const float2 saved = x.saved[at];
+  if (saved.x < 0.f) return;
   const int64_t v = x.ids[at] - (int64_t)a.vt0 * L::TILE;
   if (v < 0 || v >= (int64_t)a.n_vt * L::TILE) return;
-  float g = fast_exp2(fmaf(x.zt[at], x.z_scale, -x.lse[rowmap[c]] * LOG2E)) - share;
-  if constexpr (PER_ROW) g *= a.gam_c[c];
+  float g = fast_exp2(fmaf(saved.y, x.z_scale, -x.lse[rowmap[c]] * LOG2E)) - saved.x;
+  if constexpr (PER_ROW) g *= a.gam_c[c] * x.temperature;
   if constexpr (L::TUNED)
     *reinterpret_cast<T*>(reinterpret_cast<char*>(a.G) + (int64_t)(rl >> 4) * a.ldG + (v >> 5) * 1024 + (rl & 15) * 64 + (v & 31) * 2) = Pack4<T>::one(g);
   else

@@ -19,6 +19,7 @@ hipError_t distill_recompute(const RecomputeArgs<T>& a, int grid, const DistillL
   RecomputeTempArgs<T> x;
   static_cast<RecomputeArgs<T>&>(x) = a;
   x.z_scale = lists.z_scale;
+  x.temperature = lists.temperature;
   const unsigned blocks = (unsigned)ceil_div((int64_t)a.n_nt * L::TILE * lists.K, 256);
   if (per_row) {
     recompute_kernel<T, L, L::TUNED, true, true><<<grid, L::THREADS, L::LDS, st>>>(x);
@@ -44,9 +45,8 @@ namespace {
 
 struct DistillPlan {
   Plan p;
-  int tile, n_blk;
+  int tile, n_blk, n_win;
   int64_t off_blk_loss, off_blk_cnt, off_blk_oor, off_part, off_begin, off_entries, off_HT, fwd_bytes;
-  int64_t off_share, off_target, off_grad, off_grad_rows, bwd_bytes;
 };
 
 bool make_distill_plan(int parts, int64_t N, int64_t d, int64_t V, int64_t K, flce_dtype dt, DistillPlan& x) {
@@ -55,27 +55,29 @@ bool make_distill_plan(int parts, int64_t N, int64_t d, int64_t V, int64_t K, fl
   if (parts & PLAN_FORWARD) {
     x.tile = p.esize == 2 && !p.fast ? TILE : p.fwd_tile;
     x.n_blk = (int)ceil_div(N, DISTILL_ROWS);
+    // The cross-entropy's windows, but in fp32 where they leave CUs idle as many as give every CU two workgroups, down to a tile each
+    // (its 64-row tiles are planned by 256 positions: 256 x 256 x 4096, 256 tiles of which 64 workgroups took four each, WIN_US us).
+    const int64_t rt = ceil_div(N, x.tile), vt = ceil_div(V, x.tile);
+    x.n_win = p.n_win;
+    if (p.esize == 4 && rt * x.n_win < 2 * NUM_CU) x.n_win = (int)std::min(vt, std::max<int64_t>(x.n_win, ceil_div(2 * NUM_CU, rt)));
     const int64_t n_rt = ceil_div(N, x.tile), n_vt = ceil_div(V, x.tile);
     int64_t o = ALIGN;
     x.off_blk_loss = o; o = align_up(o + (int64_t)x.n_blk * 4, ALIGN);
     x.off_blk_cnt = o;  o = align_up(o + (int64_t)x.n_blk * 4, ALIGN);
     x.off_blk_oor = o;  o = align_up(o + (int64_t)x.n_blk * 4, ALIGN);
-    x.off_part = o;     o = align_up(o + 2ll * p.n_win * p.npad * 4, ALIGN);
+    x.off_part = o;     o = align_up(o + 2ll * x.n_win * p.npad * 4, ALIGN);
     x.off_begin = o;    o = align_up(o + n_rt * (n_vt + 1) * 4, ALIGN);
     x.off_entries = o;  o = align_up(o + n_rt * x.tile * K * 4, ALIGN);
     x.off_HT = o;       if (p.fwd_copy) o = align_up(o + packed_block_offset(p.n_rb, (int)d), ALIGN);
     x.fwd_bytes = o;
   }
-  if (parts & PLAN_BACKWARD) {
-    int64_t o = align_up(p.bwd_bytes, ALIGN);
-    x.off_share = o;     o = align_up(o + N * K * 4, ALIGN);
-    x.off_target = o;    o = align_up(o + N * 8, ALIGN);
-    x.off_grad = o;      o += ALIGN;
-    x.off_grad_rows = o; o = align_up(o + N * 4, ALIGN);
-    x.bwd_bytes = o;
-  }
   return true;
 }
+
+// What the forward leaves for the backward: targets, then (share, logit) per list entry.
+int64_t saved_bytes(int64_t N, int64_t K) { return align_up(N * 8, ALIGN) + N * K * 8; }
+int64_t* saved_targets(void* saved) { return static_cast<int64_t*>(saved); }
+float2* saved_entries(void* saved, int64_t N) { return reinterpret_cast<float2*>(static_cast<char*>(saved) + align_up(N * 8, ALIGN)); }
 
 template <typename T, typename L>
 hipError_t distill_tiles_allowance() {
@@ -102,22 +104,29 @@ extern "C" {
 size_t flce_distill_workspace_bytes(int64_t N, int64_t d, int64_t V, int64_t K, flce_dtype dt, int for_backward) {
   flce::DistillPlan x;
   if (!flce::make_distill_plan(for_backward ? flce::PLAN_BACKWARD : flce::PLAN_FORWARD, N, d, V, K, dt, x)) return 0;
-  return (size_t)(for_backward ? x.bwd_bytes : x.fwd_bytes);
+  return (size_t)(for_backward ? x.p.bwd_bytes : x.fwd_bytes);
+}
+
+size_t flce_distill_saved_bytes(int64_t N, int64_t K) {
+  if (N < 1 || N > 0x7FFFFF00ll || K < 1 || K > flce::DISTILL_MAX) return 0;
+  return (size_t)flce::saved_bytes(N, K);
 }
 
 flce_status flce_distill_forward(const void* H, const void* W, const int64_t* teacher_ids, const float* teacher_logits, int64_t N, int64_t d,
                                  int64_t V, int64_t K, float temperature, flce_reduction reduction, flce_dtype dt, float* loss_out,
-                                 float* loss_rows_out, float* lse_out, float* zt_out, void* workspace, size_t workspace_bytes,
+                                 float* loss_rows_out, float* lse_out, void* saved_out, void* workspace, size_t workspace_bytes,
                                  void* hip_stream) {
   using namespace flce;
-  if (!H || !W || !teacher_ids || !teacher_logits || (!loss_out && !loss_rows_out) || !lse_out || !zt_out) return FLCE_ERR_BAD_ARG;
+  if (!H || !W || !teacher_ids || !teacher_logits || (!loss_out && !loss_rows_out) || !lse_out || !saved_out) return FLCE_ERR_BAD_ARG;
   if (reduction != FLCE_REDUCE_MEAN && reduction != FLCE_REDUCE_SUM) return FLCE_ERR_BAD_ARG;
   if (dt != FLCE_DTYPE_BF16 && dt != FLCE_DTYPE_F32) return FLCE_ERR_BAD_ARG;
   if (!temperature_ok(temperature)) return FLCE_ERR_BAD_ARG;
   DistillPlan x;
   if (!make_distill_plan(PLAN_FORWARD, N, d, V, K, dt, x)) return FLCE_ERR_BAD_SHAPE;
-  if (!aligned16(H) || !aligned16(W)) return FLCE_ERR_BAD_ARG;
+  if (!aligned16(H) || !aligned16(W) || !aligned16(saved_out)) return FLCE_ERR_BAD_ARG;
   if (bad_workspace(workspace, workspace_bytes, x.fwd_bytes)) return FLCE_ERR_WORKSPACE;
+  int64_t* target = saved_targets(saved_out);
+  float2* saved = saved_entries(saved_out, N);
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   char* ws = static_cast<char*>(workspace);
   const Plan& p = x.p;
@@ -131,11 +140,11 @@ flce_status flce_distill_forward(const void* H, const void* W, const int64_t* te
     using T = typename decltype(tag)::T;
     using L = typename decltype(tag)::L;
     if (distill_tiles_allowance<T, L>() != hipSuccess) return FLCE_ERR_HIP;
-    const int n_rb = (int)ceil_div(N, L::TILE), n_vt = (int)ceil_div(V, L::TILE), items = n_rb * p.n_win;
+    const int n_rb = (int)ceil_div(N, L::TILE), n_vt = (int)ceil_div(V, L::TILE), items = n_rb * x.n_win;
     {
       ProfScope ps(FLCE_PROF_FWD_EPILOGUE, st);
       distill_lists_kernel<L::TILE><<<(unsigned)n_rb, 1024, 0, st>>>(teacher_ids, teacher_logits, (int)N, (int)V, (int)K, n_vt, begin, entries,
-                                                                     zt_out, hdr);
+                                                                     saved, hdr);
     }
     {
       // one workgroup per (row block, window), with the tuned loop a round of them per launch, as the cross-entropy's forward
@@ -144,8 +153,8 @@ flce_status flce_distill_forward(const void* H, const void* W, const int64_t* te
       if constexpr (L::TUNED) per_launch = NUM_CU * L::PER_CU;
       for (int item0 = 0; item0 < items; item0 += per_launch) {
         const DistillTileArgs<T> a{static_cast<const T*>(H), static_cast<const T*>(HT), static_cast<const T*>(W), (int)N, (int)d, (int)V, n_rb,
-                                   p.n_win, n_vt, (double)n_vt / p.n_win, LOG2E / temperature, part, p.npad, item0, begin, entries, (int)K,
-                                   zt_out};
+                                   x.n_win, n_vt, (double)n_vt / x.n_win, LOG2E / temperature, part, p.npad, item0, begin, entries, (int)K,
+                                   saved};
         const int grid = std::min(per_launch, items - item0);
         if constexpr (L::TUNED) {
           if (HT) { distill_tiles_kernel<T, L, true><<<grid, L::THREADS, L::LDS, st>>>(a); continue; }
@@ -157,7 +166,7 @@ flce_status flce_distill_forward(const void* H, const void* W, const int64_t* te
     // a call for rows alone has no scalar loss to hand out: the sum goes to a spare word of the header block
     float* scalar = loss_out ? loss_out : reinterpret_cast<float*>(ws + 64);
     distill_rows_kernel<<<x.n_blk, 64 * DISTILL_ROWS, 0, st>>>(DistillRowArgs{
-        teacher_ids, teacher_logits, zt_out, (int)N, (int)V, (int)K, p.n_win, part, p.npad, temperature, 1.f / temperature,
+        teacher_ids, teacher_logits, saved, target, (int)N, (int)V, (int)K, x.n_win, part, p.npad, temperature, 1.f / temperature,
         LOG2E / temperature, lse_out, loss_rows_out,
         LossOut{reinterpret_cast<float*>(ws + x.off_blk_loss), reinterpret_cast<int*>(ws + x.off_blk_cnt),
                 reinterpret_cast<int*>(ws + x.off_blk_oor), hdr, scalar, reduction == FLCE_REDUCE_MEAN, nullptr, nullptr}});
@@ -165,37 +174,19 @@ flce_status flce_distill_forward(const void* H, const void* W, const int64_t* te
   });
 }
 
-flce_status flce_distill_backward(const void* H, const void* W, const int64_t* teacher_ids, const float* teacher_logits, const float* lse,
-                                  const float* zt, int64_t N, int64_t d, int64_t V, int64_t K, float temperature, flce_reduction reduction,
-                                  flce_dtype dt, const float* grad_loss, const float* grad_rows, void* dH_out, void* dW_out,
-                                  void* workspace, size_t workspace_bytes, void* hip_stream) {
+flce_status flce_distill_backward(const void* H, const void* W, const int64_t* teacher_ids, const float* lse, const void* saved, int64_t N,
+                                  int64_t d, int64_t V, int64_t K, float temperature, flce_reduction reduction, flce_dtype dt,
+                                  const float* grad_loss, const float* grad_rows, void* dH_out, void* dW_out, void* workspace,
+                                  size_t workspace_bytes, void* hip_stream) {
   using namespace flce;
-  if (!H || !W || !teacher_ids || !teacher_logits || !lse || !zt || !dH_out || !dW_out) return FLCE_ERR_BAD_ARG;
-  if (!grad_loss == !grad_rows) return FLCE_ERR_BAD_ARG;
-  if (reduction != FLCE_REDUCE_MEAN && reduction != FLCE_REDUCE_SUM) return FLCE_ERR_BAD_ARG;
-  if (dt != FLCE_DTYPE_BF16 && dt != FLCE_DTYPE_F32) return FLCE_ERR_BAD_ARG;
-  if (!temperature_ok(temperature)) return FLCE_ERR_BAD_ARG;
-  DistillPlan x;
-  if (!make_distill_plan(PLAN_BACKWARD, N, d, V, K, dt, x)) return FLCE_ERR_BAD_SHAPE;
-  if (!aligned16(H) || !aligned16(W) || !aligned16(dH_out) || !aligned16(dW_out)) return FLCE_ERR_BAD_ARG;
-  if (bad_workspace(workspace, workspace_bytes, x.bwd_bytes)) return FLCE_ERR_WORKSPACE;
-  hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  char* ws = static_cast<char*>(workspace);
-  float* share = reinterpret_cast<float*>(ws + x.off_share);
-  int64_t* target = reinterpret_cast<int64_t*>(ws + x.off_target);
-  float* grad = reinterpret_cast<float*>(ws + x.off_grad);
-  float* grad_n = reinterpret_cast<float*>(ws + x.off_grad_rows);
-  {
-    ProfScope ps(FLCE_PROF_BWD_PREP, st);
-    distill_prep_kernel<<<(unsigned)ceil_div(N, DISTILL_ROWS), 64 * DISTILL_ROWS, 0, st>>>(
-        DistillPrepArgs{teacher_ids, teacher_logits, (int)N, (int)V, (int)K, 1.f / temperature, temperature, share, target, grad_loss,
-                        grad_rows, grad, grad_n});
-  }
-  const DistillLists lists{teacher_ids, share, zt, lse, (int)K, LOG2E / temperature};
+  if (!teacher_ids || !saved || !aligned16(saved) || !grad_loss == !grad_rows || !temperature_ok(temperature)) return FLCE_ERR_BAD_ARG;
+  if (!flce_distill_saved_bytes(N, K)) return FLCE_ERR_BAD_SHAPE;
+  void* s = const_cast<void*>(saved);       // (read only)
+  const DistillLists lists{teacher_ids, saved_entries(s, N), lse, (int)K, temperature, LOG2E / temperature};
   // one vocabulary position more than W has: the targets of rows that count lie there
-  return backward_impl(H, W, target, lse, N, d, V, -1, grad_rows ? FLCE_REDUCE_SUM : reduction, dt,
-                       grad_rows ? GradLoss{1.f, nullptr} : GradLoss{0.f, grad}, dH_out, dW_out, workspace, workspace_bytes, hip_stream,
-                       Slice{V + 1, 0}, PerRow{nullptr, grad_rows ? grad_n : nullptr, 0.f}, &lists);
+  return backward_impl(H, W, saved_targets(s), lse, N, d, V, -1, grad_rows ? FLCE_REDUCE_SUM : reduction, dt,
+                       grad_rows ? GradLoss{1.f, nullptr} : GradLoss{temperature, grad_loss}, dH_out, dW_out, workspace, workspace_bytes,
+                       hip_stream, Slice{V + 1, 0}, PerRow{nullptr, grad_rows, 0.f}, &lists);
 }
 
 }  // extern "C"

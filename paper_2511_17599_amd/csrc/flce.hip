@@ -963,7 +963,7 @@ flce_status flce_backward_device_grad(const void* H, const void* W, const int64_
                                       const float* grad_loss, void* dH_out, void* dW_out, void* workspace,
                                       size_t workspace_bytes, void* hip_stream) {
   if (!grad_loss) return FLCE_ERR_BAD_ARG;
-  return flce::backward_impl(H, W, targets, lse, N, d, V, ignore_index, reduction, dt, flce::GradLoss{0.f, grad_loss}, dH_out,
+  return flce::backward_impl(H, W, targets, lse, N, d, V, ignore_index, reduction, dt, flce::GradLoss{1.f, grad_loss}, dH_out,
                        dW_out, workspace, workspace_bytes, hip_stream, flce::Slice{V, 0});
 }
 

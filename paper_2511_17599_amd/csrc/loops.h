@@ -264,10 +264,10 @@ __device__ __forceinline__ V wave_sum(V v) {
   return v;
 }
 
-// Upstream gradient of the scalar loss: a device word if there is one, a host value otherwise.
+// Upstream gradient of the scalar loss: a device word times a host factor if there is one, the host value otherwise.
 struct GradLoss {
   float value; const float* word;
-  __device__ __forceinline__ float get() const { return word ? *word : value; }
+  __device__ __forceinline__ float get() const { return word ? *word * value : value; }
 };
 
 // Where the reduced loss of a call goes.

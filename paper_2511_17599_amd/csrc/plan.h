@@ -76,14 +76,13 @@ struct StatusOut { int32_t* status; int64_t* n_valid; };
 // The forward's pre-tiled copy of H (p.npad rows, zero behind the last one).
 void pack_rows(const Plan& p, const void* H, void* HT, hipStream_t st);
 
-// What a distillation's backward has beside the cross-entropy's: lists of K entries per row, logits at them and shares.
+// What a distillation's backward has beside the cross-entropy's: lists of K entries per row, shares and the logits at them.
 struct DistillLists {
   const int64_t* ids;     // [N][K]
-  const float* share;     // [N][K]: the teacher's probability of the id at its first place in a row, negative elsewhere
-  const float* zt;        // [N][K]: the student's logit
+  const float2* saved;    // [N][K]: the teacher's share of the id at its first place in a row, negative elsewhere; the student's logit
   const float* lse;       // [N], of the logits / temperature
   int K;
-  float z_scale;          // log2(e) / temperature
+  float temperature, z_scale;          // log2(e) / temperature
 };
 // The recompute step of one chunk with those: G = softmax(z / temperature) - share (times the row's gradient if per_row).
 template <typename T, typename L>

@@ -30,6 +30,7 @@ struct RecomputeArgs {
 template <typename T>
 struct RecomputeTempArgs : RecomputeArgs<T> {
   float z_scale;        // log2(e) / temperature
+  float temperature;    // PER_ROW: G = temperature * Gamma_row * (p - ...)
 };
 
 // Per-row inputs of a recompute tile, one set per token column a lane owns.
@@ -131,6 +132,7 @@ __global__ __launch_bounds__(L::THREADS, L::MIN_WAVES) void recompute_kernel(
         const float ll = tgt >= 0 ? -meta.lse[j] * LOG2E : NEG_INF;
         float gam = 1.f;
         if constexpr (PER_ROW) gam = tgt >= 0 ? meta.gam[j] : 0.f;
+        if constexpr (PER_ROW && TEMP) gam *= a.temperature;
         const float unif = tgt >= 0 ? a.uniform_part : 0.f;
         // A whole column of blocks without a target of the wavefront and inside the vocabulary (almost all are: POS of V
         // positions) needs no tests (step of 4326 x 232 x 74697 1044 -> 1008 us, 1144 x 576 x 191782 1306 -> 1264,
@@ -219,6 +221,7 @@ __global__ __launch_bounds__(L::THREADS, L::MIN_WAVES) void recompute_kernel(
         const float ll = tgt >= 0 ? -meta.lse[j] * LOG2E : NEG_INF;
         float gam = 1.f;
         if constexpr (PER_ROW) gam = tgt >= 0 ? meta.gam[j] : 0.f;
+        if constexpr (PER_ROW && TEMP) gam *= a.temperature;
         const float unif = tgt >= 0 ? a.uniform_part : 0.f;
         // Does any token column of this wavefront have its target among the block's 32 vocabulary positions?
         // Almost never (32 of V positions), and then the one-hot term costs nothing: a wave-uniform branch.

@@ -18,7 +18,7 @@ On a few logits per row:
 """
 from __future__ import annotations
 
-import contextlib
+import functools
 import weakref
 
 import torch
@@ -159,9 +159,14 @@ def linear_cross_entropy(H, W, targets, ignore_index=-100, reduction="mean", lab
     return _RowLosses.apply(H, W, targets, int(ignore_index), float(label_smoothing))
 
 
-def _on_device(device):
+def _launch(call, device, *args):
     """The library launches on the current device: the tensors' own, whichever is current for the caller."""
-    return contextlib.nullcontext() if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+    if torch.cuda.current_device() == device.index:
+        rc = call(*args, _stream(device))
+    else:
+        with torch.cuda.device(device):
+            rc = call(*args, _stream(device))
+    _check(rc)
 
 
 def _operands(H, W):
@@ -173,15 +178,14 @@ def _operands(H, W):
         raise ValueError("H and W are on different devices")
     if H.dim() < 1 or W.dim() != 2 or W.shape[1] != H.shape[-1]:
         raise ValueError("shapes: H [..., d], W [V, d]")
-    return H.reshape(-1, H.shape[-1]).contiguous(), W.contiguous()
+    return H if H.dim() == 2 and H.is_contiguous() else H.reshape(-1, H.shape[-1]).contiguous(), W.contiguous()
 
 
-def _beside(H, dtype, **tensors):
-    """Further arguments as the library wants them: H's device, contiguous, of one type."""
-    for name, t in tensors.items():
-        if t.device != H.device:
-            raise ValueError(f"{name} is on another device than H")
-        yield t.to(dtype).contiguous()
+def _beside(device, t, dtype, name):
+    """A further argument as the library wants it: on H's device, contiguous, of one type."""
+    if t.device != device:
+        raise ValueError(f"{name} is on another device than H")
+    return t if t.dtype is dtype and t.is_contiguous() else t.to(dtype).contiguous()
 
 
 def _scratch(nbytes, device, what):
@@ -205,8 +209,9 @@ def linear_topk(H, W, k):
         logits = torch.empty(N, k, dtype=torch.float32, device=dev)
         ids = torch.empty(N, k, dtype=torch.int64, device=dev)
         lse = torch.empty(N, dtype=torch.float32, device=dev)
-        with _on_device(dev):
-            _check(B.flce_topk(H2, W2, N, d, V, k, dt, logits, ids, lse, ws, nb, _stream(dev)))
+        _launch(B.flce_topk, dev, H2, W2, N, d, V, k, dt, logits, ids, lse, ws, nb)
+    if H.dim() == 2:
+        return logits, ids, lse
     lead = H.shape[:-1]
     return logits.reshape(*lead, k), ids.reshape(*lead, k), lse.reshape(lead)
 
@@ -245,41 +250,43 @@ class _Distillation(torch.autograd.Function):
         H2, W2 = _operands(H, W)
         (N, d), V, dt, dev = H2.shape, W2.shape[0], _DT[H2.dtype], H2.device
         K = ids.shape[-1]
-        ids2, = _beside(H2, torch.int64, teacher_ids=ids.reshape(-1, K))
-        t2, = _beside(H2, torch.float32, teacher_logits=logits.reshape(-1, K))
+        ids2 = _beside(dev, ids, torch.int64, "teacher_ids")
+        t2 = _beside(dev, logits, torch.float32, "teacher_logits")
         ws, nb = _scratch(B.flce_distill_workspace_bytes(N, d, V, K, dt, 0), dev,
                           "d must be a multiple of 8, 1 <= K <= 256, at least one row")
         rows = reduction == "none"
-        out = torch.empty(N if rows else (), dtype=torch.float32, device=dev)
-        lse = torch.empty(N, dtype=torch.float32, device=dev)
-        zt = torch.empty(N, K, dtype=torch.float32, device=dev)
-        with _on_device(dev):
-            _check(B.flce_distill_forward(H2, W2, ids2, t2, N, d, V, K, temperature, _RED.get(reduction, B.FLCE_REDUCE_SUM), dt,
-                                          None if rows else out, out if rows else None, lse, zt, ws, nb, _stream(dev)))
-        ctx.save_for_backward(H2, W2, ids2, t2, lse, zt)
-        ctx.meta = (H.shape, temperature, reduction)
+        out = torch.empty(H.shape[:-1] if rows else (), dtype=torch.float32, device=dev)
+        ns = B.flce_distill_saved_bytes(N, K)
+        keep = torch.empty(ns + 4 * N, dtype=torch.uint8, device=dev)        # what the backward takes, lse behind it
+        saved = keep.data_ptr()
+        _launch(B.flce_distill_forward, dev, H2, W2, ids2, t2, N, d, V, K, temperature, _RED.get(reduction, B.FLCE_REDUCE_SUM), dt,
+                None if rows else out, out if rows else None, saved + ns, saved, ws, nb)
+        ctx.save_for_backward(H2, W2, ids2, keep)
+        ctx.meta = (H.shape, temperature, reduction, K, ns)
         ctx.graph = graph
-        return out.reshape(H.shape[:-1]) if rows else out
+        return out
 
     @staticmethod
     def backward(ctx, grad):
-        H2, W2, ids2, t2, lse, zt = ctx.saved_tensors
-        shape, temperature, reduction = ctx.meta
-        (N, d), V, K, dt, dev = H2.shape, W2.shape[0], ids2.shape[1], _DT[H2.dtype], H2.device
+        H2, W2, ids2, keep = ctx.saved_tensors
+        shape, temperature, reduction, K, ns = ctx.meta
+        (N, d), V, dt, dev = H2.shape, W2.shape[0], _DT[H2.dtype], H2.device
         # The kernels read the gradient where it is; one that is only marked as negated or zero is made first.
-        g = grad.to(device=dev, dtype=torch.float32)
+        g = grad
+        if g.dtype is not torch.float32 or g.device != dev:
+            g = g.to(device=dev, dtype=torch.float32)
         if g.is_neg() or g._is_zerotensor():
             g = g.clone().resolve_neg()
         rows = reduction == "none"
         if rows:
-            g = g.reshape(-1).contiguous()
+            g = g.contiguous()
         dH = torch.empty_like(H2)
         dW = torch.empty_like(W2)
         ws, nb = _scratch(B.flce_distill_workspace_bytes(N, d, V, K, dt, 1), dev, "as in the forward")
-        with _on_device(dev):
-            _check(B.flce_distill_backward(H2, W2, ids2, t2, lse, zt, N, d, V, K, temperature, _RED.get(reduction, B.FLCE_REDUCE_SUM),
-                                           dt, None if rows else g, g if rows else None, dH, dW, ws, nb, _stream(dev)))
-        return dH.reshape(shape), dW, None, None, None, None, None
+        saved = keep.data_ptr()
+        _launch(B.flce_distill_backward, dev, H2, W2, ids2, saved + ns, saved, N, d, V, K, temperature,
+                _RED.get(reduction, B.FLCE_REDUCE_SUM), dt, None if rows else g, g if rows else None, dH, dW, ws, nb)
+        return dH if dH.shape == shape else dH.reshape(shape), dW, None, None, None, None, None
 
 
 def linear_distillation(H, W, teacher_ids, teacher_logits, temperature=1.0, reduction="mean"):
@@ -298,7 +305,7 @@ def linear_distillation(H, W, teacher_ids, teacher_logits, temperature=1.0, redu
         raise TypeError("teacher_ids are integers, teacher_logits are floating point")
     if teacher_ids.shape != teacher_logits.shape or teacher_ids.dim() != H.dim() or teacher_ids.shape[:-1] != H.shape[:-1]:
         raise ValueError("shapes: H [..., d], teacher_ids and teacher_logits [..., K]")
-    return _Distillation.apply(H, W, teacher_ids, teacher_logits.detach(), float(temperature), reduction, _graph_of(H, W))
+    return _Distillation.apply(H, W, teacher_ids, teacher_logits, float(temperature), reduction, _graph_of(H, W))
 
 
 def beam_step(H, W, scores, finished=None, n_out=None, eos_id=-1, pad_id=0):
@@ -314,17 +321,36 @@ def beam_step(H, W, scores, finished=None, n_out=None, eos_id=-1, pad_id=0):
         H2, W2 = _operands(H.detach(), W.detach())
         (batch, beams, d), V, dt, dev = H.shape, W2.shape[0], _DT[H2.dtype], H2.device
         n_out = beams if n_out is None else int(n_out)
-        s, = _beside(H2, torch.float32, scores=scores.detach())
-        f = None
-        if finished is not None:
-            f, = _beside(H2, torch.bool, finished=finished)
+        s = _beside(dev, scores, torch.float32, "scores")
+        f = None if finished is None else _beside(dev, finished, torch.bool, "finished")
         ws, nb = _scratch(B.flce_beam_workspace_bytes(batch, beams, d, V, n_out, dt), dev,
                           "d must be a multiple of 8, beams and n_out 1 .. 64, V <= 2^22, at least one search")
         out = (torch.empty(batch, n_out, dtype=torch.float32, device=dev), torch.empty(batch, n_out, dtype=torch.int64, device=dev),
                torch.empty(batch, n_out, dtype=torch.int64, device=dev), torch.empty(batch, n_out, dtype=torch.bool, device=dev))
-        with _on_device(dev):
-            _check(B.flce_beam_step(H2, W2, s, f, batch, beams, d, V, n_out, int(eos_id), int(pad_id), dt, *out, ws, nb, _stream(dev)))
+        _launch(B.flce_beam_step, dev, H2, W2, s, f, batch, beams, d, V, n_out, int(eos_id), int(pad_id), dt, *out, ws, nb)
     return out
+
+
+@functools.lru_cache(1024)
+def _rows_of(shape, stride, dim, size):
+    """(bytes of a beam's row, number of outer slabs, bytes from row to row, bytes from slab to slab) of a states tensor."""
+    run = 1
+    for n, s in zip(shape[:dim + 1:-1], stride[:dim + 1:-1]):
+        if n > 1 and s != run:
+            raise ValueError("a beam's state must be contiguous")
+        run *= n
+    batch, beams = shape[dim], shape[dim + 1]
+    row = stride[dim + 1] if beams > 1 else stride[dim] if batch > 1 else run
+    if batch > 1 and stride[dim] != beams * row:
+        raise ValueError("batch and beams must be one run of rows")
+    outer, step = 1, None
+    for n, s in zip(shape[:dim][::-1], stride[:dim][::-1]):
+        if n > 1:
+            if step is not None and s != step * outer:
+                raise ValueError("the dimensions ahead of the batch must be strided once")
+            step = s if step is None else step
+            outer *= n
+    return run * size, outer, row * size, (step or 0) * size
 
 
 def reorder_states(parents, states, out=None, dim=1, status=None):
@@ -351,29 +377,8 @@ def reorder_states(parents, states, out=None, dim=1, status=None):
     if out.numel() == 0:
         return out
 
-    def strides(t):
-        """Bytes from row to row and from outer to outer."""
-        size, run = t.element_size(), 1
-        for n, s in zip(reversed(t.shape[dim + 2:]), reversed(t.stride()[dim + 2:])):
-            if n > 1 and s != run:
-                raise ValueError("a beam's state must be contiguous")
-            run *= n
-        row = t.stride(dim + 1) if t.shape[dim + 1] > 1 else (t.stride(dim) if batch > 1 else run)
-        if batch > 1 and t.stride(dim) != t.shape[dim + 1] * row:
-            raise ValueError("batch and beams must be one run of rows")
-        outer, step = 1, None
-        for n, s in zip(reversed(t.shape[:dim]), reversed(t.stride()[:dim])):
-            if n > 1:
-                if step is not None and s != step * outer:
-                    raise ValueError("the dimensions ahead of the batch must be strided once")
-                step = s if step is None else step
-                outer *= n
-        return run * size, outer, row * size, (step or 0) * size
-
-    row_bytes, outer, src_row, src_outer = strides(states)
-    _, _, dst_row, dst_outer = strides(out)
-    p = parents.to(torch.int64).contiguous()
-    with _on_device(states.device):
-        _check(B.flce_beam_reorder(states, out, p, outer, batch, beams_in, beams_out, row_bytes, src_row, src_outer, dst_row, dst_outer,
-                                   status, _stream(states.device)))
+    row_bytes, outer, src_row, src_outer = _rows_of(states.shape, states.stride(), dim, states.element_size())
+    _, _, dst_row, dst_outer = _rows_of(want, out.stride(), dim, out.element_size())
+    _launch(B.flce_beam_reorder, states.device, states, out, _beside(states.device, parents, torch.int64, "parents"), outer, batch, beams_in,
+            beams_out, row_bytes, src_row, src_outer, dst_row, dst_outer, status)
     return out

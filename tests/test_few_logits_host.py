@@ -35,22 +35,22 @@ def test_topk_workspace():
         assert B.flce_topk_workspace_bytes(N, 4096, 128256, 64, BF16) < (1 << 30) * 1.05 + N * 4096 * 2 * 1.01 + (1 << 20)
 
 
-def fwd(H=P, W=P, ids=P, t=P, N=8, d=64, V=512, K=4, T=1.0, red=0, dt=F32, loss=P, rows=None, lse=P, zt=P, ws=P, nb=1 << 40):
-    return B.flce_distill_forward(H, W, ids, t, N, d, V, K, T, red, dt, loss, rows, lse, zt, ws, nb)
+def fwd(H=P, W=P, ids=P, t=P, N=8, d=64, V=512, K=4, T=1.0, red=0, dt=F32, loss=P, rows=None, lse=P, saved=P, ws=P, nb=1 << 40):
+    return B.flce_distill_forward(H, W, ids, t, N, d, V, K, T, red, dt, loss, rows, lse, saved, ws, nb)
 
 
-def bwd(H=P, W=P, ids=P, t=P, lse=P, zt=P, N=8, d=64, V=512, K=4, T=1.0, red=0, dt=F32, g=P, gr=None, dH=P, dW=P, ws=P, nb=1 << 40):
-    return B.flce_distill_backward(H, W, ids, t, lse, zt, N, d, V, K, T, red, dt, g, gr, dH, dW, ws, nb)
+def bwd(H=P, W=P, ids=P, lse=P, saved=P, N=8, d=64, V=512, K=4, T=1.0, red=0, dt=F32, g=P, gr=None, dH=P, dW=P, ws=P, nb=1 << 40):
+    return B.flce_distill_backward(H, W, ids, lse, saved, N, d, V, K, T, red, dt, g, gr, dH, dW, ws, nb)
 
 
-COMMON = [(dict(H=None), ARG), (dict(W=None), ARG), (dict(ids=None), ARG), (dict(t=None), ARG), (dict(lse=None), ARG), (dict(zt=None), ARG),
+COMMON = [(dict(H=None), ARG), (dict(W=None), ARG), (dict(ids=None), ARG), (dict(lse=None), ARG), (dict(saved=None), ARG), (dict(saved=P + 8), ARG),
           (dict(red=2), ARG), (dict(dt=-1), ARG), (dict(H=P + 8), ARG), (dict(T=0.0), ARG), (dict(T=-1.0), ARG),
           (dict(T=float("nan")), ARG), (dict(T=float("inf")), ARG), (dict(T=1e-40), ARG), (dict(T=1e30), ARG), (dict(K=0), SHAPE),
           (dict(K=257), SHAPE), (dict(N=0), SHAPE), (dict(d=4), SHAPE), (dict(V=-1), SHAPE), (dict(ws=None), WS), (dict(ws=P + 128), WS),
           (dict(nb=300), WS)]
 
 
-@pytest.mark.parametrize("kw,want", COMMON + [(dict(loss=None), ARG)])
+@pytest.mark.parametrize("kw,want", COMMON + [(dict(loss=None), ARG), (dict(t=None), ARG)])
 def test_distill_forward_refuses(kw, want):
     assert fwd(**kw) == want
 
@@ -70,7 +70,9 @@ def test_distill_workspaces():
     # the copy of H, the lists, a few words per row
     N, d, V, K = 131072, 4096, 128256, 32
     assert B.flce_distill_workspace_bytes(N, d, V, K, BF16, 0) < N * d * 2 * 1.01 + N * K * 4 + (64 << 20)
-    assert B.flce_distill_workspace_bytes(N, d, V, K, BF16, 1) < B.flce_workspace_bytes(N, d, V, BF16, 1) + N * (4 * K + 16) + 4096
+    assert B.flce_distill_workspace_bytes(N, d, V, K, BF16, 1) == B.flce_workspace_bytes(N, d, V, BF16, 1)
+    assert 8 * N * (K + 1) <= B.flce_distill_saved_bytes(N, K) < 8 * N * (K + 1) + 256
+    assert B.flce_distill_saved_bytes(0, 4) == B.flce_distill_saved_bytes(4, 0) == B.flce_distill_saved_bytes(4, 257) == 0
 
 
 def step(H=P, W=P, s=P, f=None, batch=2, beams=4, d=64, V=512, n_out=4, dt=F32, so=1 << 20, to=P, po=P, fo=1 << 21, ws=P, nb=1 << 40):

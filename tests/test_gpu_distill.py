@@ -46,21 +46,24 @@ def call(H, W, ids, t, T, reduction="mean", grad=1.0, grad_rows=None, stream=Non
     dt = CODE["bf16" if H.dtype is torch.bfloat16 else "f32"]
     red = {"mean": B.FLCE_REDUCE_MEAN, "sum": B.FLCE_REDUCE_SUM}[reduction]
     f = lambda *s: torch.full(s, 7.0, device="cuda")
-    loss, rows, lse, zt = f(1), f(N + 16), f(N + 16), f(N * K + 16)
+    loss, rows, lse = f(1), f(N + 16), f(N + 16)
     nf, nb = (B.flce_distill_workspace_bytes(N, d, V, K, dt, b) for b in (0, 1))
-    wf, wb = (torch.full((n + 64,), 0xFF, dtype=torch.uint8, device="cuda") for n in (nf, nb))
+    ns = B.flce_distill_saved_bytes(N, K)
+    wf, wb, saved = (torch.full((n + 64,), 0xFF, dtype=torch.uint8, device="cuda") for n in (nf, nb, ns))
     dH, dW = torch.full((N * d + 64,), 7.0, dtype=H.dtype, device="cuda"), torch.full((V * d + 64,), 7.0, dtype=H.dtype, device="cuda")
-    assert B.flce_distill_forward(H, W, ids, t, N, d, V, K, T, red, dt, loss, rows, lse, zt, wf, nf, stream) == B.FLCE_OK
+    assert B.flce_distill_forward(H, W, ids, t, N, d, V, K, T, red, dt, loss, rows, lse, saved, wf, nf, stream) == B.FLCE_OK
     status = B.flce_last_device_status(wf, stream)
     up = None if grad_rows is not None else torch.full((1,), grad, device="cuda")
     torch.cuda.synchronize()
-    assert B.flce_distill_backward(H, W, ids, t, lse, zt, N, d, V, K, T, red, dt, up, grad_rows, dH, dW, wb, nb, stream) == B.FLCE_OK
+    kept = saved.clone()
+    assert B.flce_distill_backward(H, W, ids, lse, saved, N, d, V, K, T, red, dt, up, grad_rows, dH, dW, wb, nb, stream) == B.FLCE_OK
     assert B.flce_last_device_status(wb, stream) == status
     torch.cuda.synchronize()
-    for x in (rows[N:], lse[N:], zt[N * K:], dH[N * d:], dW[V * d:]):
+    for x in (rows[N:], lse[N:], dH[N * d:], dW[V * d:]):
         assert (x == 7).all()
-    assert (wf[nf:] == 0xFF).all() and (wb[nb:] == 0xFF).all()
-    return dict(loss=loss, rows=rows[:N], lse=lse[:N], zt=zt[:N * K].reshape(N, K), dH=dH[:N * d].reshape(N, d),
+    assert (wf[nf:] == 0xFF).all() and (wb[nb:] == 0xFF).all() and (saved[ns:] == 0xFF).all() and torch.equal(saved, kept)
+    pairs = saved[ns - 8 * N * K:ns].view(torch.float32).reshape(N, K, 2)     # (share, logit) of each entry
+    return dict(loss=loss, rows=rows[:N], lse=lse[:N], zt=pairs[..., 1], share=pairs[..., 0], dH=dH[:N * d].reshape(N, d),
                 dW=dW[:V * d].reshape(V, d), status=status)
 
 
@@ -173,7 +176,8 @@ def test_no_row_counts(dtype):
     H, W = operands(rng, 70, 64, 300, dtype)
     ids = torch.full((70, 4), -1, dtype=torch.int64, device="cuda")
     got = call(F.on_gpu(H, dtype), F.on_gpu(W, dtype), ids, torch.zeros(70, 4, device="cuda"), 1.0)
-    assert got["loss"].item() == 0 and not got["rows"].any() and not got["dH"].any() and not got["dW"].any() and not got["zt"].any()
+    assert got["loss"].item() == 0 and not got["rows"].any() and not got["dH"].any() and not got["dW"].any()
+    assert not got["zt"].any() and (got["share"] == -1).all()
     assert got["status"] == (B.FLCE_OK, 0)
 
 
