@@ -22,20 +22,39 @@ template <> struct FewMma<float> {    // element e of every lane together: K ind
   }
 };
 
-// One workgroup: 16 MB vocabulary rows (a group) by 16 NT token rows.  Its four wavefronts take every fourth K step each, so
-// that together they read 256 consecutive bytes of a row of W, and their sums are added in wavefront order through LDS.
+// f(e, p[e]) for n consecutive floats of LDS, by as wide reads as there are.
+template <int n, typename F>
+__device__ __forceinline__ void for_each_value(const float* p, F f) {
+  if constexpr (n >= 4) {
+#pragma unroll
+    for (int q = 0; q < n; q += 4) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(p + q);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f(q + e, x[e]);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < n; ++e) f(e, p[e]);
+  }
+}
+
+// One workgroup: 16 MB vocabulary rows by 16 NT token rows.  Its four wavefronts take U consecutive K steps (64 U bytes of a row of W) in
+// turn, and their sums are added in wavefront order through LDS.
 // W goes from memory to the matrix instruction's registers without a stop in LDS: no element of it is used twice by a wavefront.
-// Bound by the read of W; H (N d elements, from the L2) is read once per workgroup.
-template <typename T, int MB, int NT>
+// Bound by the read of W (128256 x 4096 in bf16, this kernel and the selection: 1 row 217 us, 32 rows 247, 64 rows 300); H (N d elements,
+// from the L2) is read once per workgroup.  Tried and no faster: a wavefront per group with H shared through LDS or the L1 (32 rows 251 to
+// 283), the next run's loads issued ahead of the products (registers for them cost more wavefronts than they gain), loads of W
+// that pass the caches (291).
+template <typename T, int MB, int NT, int U>
 __global__ __launch_bounds__(64 * FEW_WAVES) void few_rows_kernel(const T* __restrict__ H, const T* __restrict__ W, int N, int d, int V,
                                                                   float* __restrict__ z, int64_t ldz, float2* __restrict__ stats,
                                                                   int64_t ld_stats) {
-  constexpr int VEC = 16 / (int)sizeof(T), STEP = 4 * VEC, U = MB * NT >= 8 ? 2 : 4, GROUP = 16 * MB, LD = GROUP + 4;
-  constexpr int TURN = MB * NT >= 16 ? NT / 2 : NT;       // blocks of tokens that go through LDS at a time (35 KiB at most)
+  constexpr int VEC = 16 / (int)sizeof(T), STEP = 4 * VEC, GB = MB < 4 ? MB : 4, GROUP = 16 * GB, LD = GROUP + 4;
+  constexpr int TURN = GB * NT >= 16 ? NT / 2 : NT;       // blocks of tokens that go through LDS at a time (35 KiB at most)
   __shared__ __align__(16) float part[FEW_WAVES][16 * TURN][LD];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int row = lane & 15, k0 = (lane >> 4) * VEC;
-  const int v0 = blockIdx.x * GROUP;
+  const int v0 = blockIdx.x * (16 * MB);
   const T* wp[MB];
   const T* hp[NT];
 #pragma unroll
@@ -48,17 +67,15 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void few_rows_kernel(const T* __res
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  const int steps = (d + STEP - 1) / STEP, whole = d / STEP;
-  int s = wave;
-  for (; s + (U - 1) * FEW_WAVES < whole; s += U * FEW_WAVES) {
+  int k = wave * U * STEP;
+  for (; k + U * STEP <= d; k += FEW_WAVES * U * STEP) {
     u32x4 a[U][MB], b[U][NT];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int k = (s + u * FEW_WAVES) * STEP;
 #pragma unroll
-      for (int i = 0; i < MB; ++i) a[u][i] = *reinterpret_cast<const u32x4*>(wp[i] + k);
+      for (int i = 0; i < MB; ++i) a[u][i] = *reinterpret_cast<const u32x4*>(wp[i] + k + u * STEP);
 #pragma unroll
-      for (int j = 0; j < NT; ++j) b[u][j] = *reinterpret_cast<const u32x4*>(hp[j] + k);
+      for (int j = 0; j < NT; ++j) b[u][j] = *reinterpret_cast<const u32x4*>(hp[j] + k + u * STEP);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -67,8 +84,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void few_rows_kernel(const T* __res
 #pragma unroll
         for (int j = 0; j < NT; ++j) FewMma<T>::run(a[u][i], b[u][j], acc[i][j]);
   }
-  for (; s < steps; s += FEW_WAVES) {
-    const int k = s * STEP;
+  for (const int end = min(d, k + U * STEP); k < end; k += STEP) {     // the wavefront that has the last, shorter run
     const bool in = k + k0 < d;         // d is a multiple of 8: 16 bytes are inside or outside
     u32x4 a[MB], b[NT];
 #pragma unroll
@@ -80,57 +96,82 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void few_rows_kernel(const T* __res
 #pragma unroll
       for (int j = 0; j < NT; ++j) FewMma<T>::run(a[i], b[j], acc[i][j]);
   }
-  // GROUP lanes per token
-  constexpr int PER_WAVE = 64 / GROUP;
-  const int pos = lane % GROUP, v = v0 + pos;
+
+  // One group of the workgroup's and TURN blocks of tokens at a time: TPT neighbouring lanes have a token, VPT positions each.
+  constexpr int TPT = 64 * FEW_WAVES / (16 * TURN), VPT = GROUP / TPT;
+  static_assert(VPT >= 1 && (VPT & (VPT - 1)) == 0, "lanes and positions of a token");
+  const int nl = threadIdx.x / TPT, pos = threadIdx.x % TPT * VPT;
 #pragma unroll
-  for (int j0 = 0; j0 < NT; j0 += TURN) {
-    if (j0 > 0) __syncthreads();
-    // block (i, j): element r of a lane is vocabulary row 4 (l / 16) + r, token l % 16
+  for (int i0 = 0; i0 < MB; i0 += GB) {
+    const int g0 = v0 + i0 * 16;
+    if (g0 >= V) break;
 #pragma unroll
-    for (int i = 0; i < MB; ++i)
+    for (int j0 = 0; j0 < NT; j0 += TURN) {
+      if (j0 * 16 >= N) break;
+      if (i0 + j0 > 0) __syncthreads();
+      // block (i, j): element r of a lane is vocabulary row 4 (l / 16) + r, token l % 16
 #pragma unroll
-      for (int j = 0; j < TURN; ++j)
-        *reinterpret_cast<f32x4*>(&part[wave][j * 16 + row][i * 16 + (lane >> 4) * 4]) = acc[i][j0 + j];
-    __syncthreads();
-#pragma unroll 4
-    for (int nl = wave * PER_WAVE; nl < 16 * TURN; nl += FEW_WAVES * PER_WAVE) {
-      if (j0 * 16 + nl >= N) break;
-      const int n = j0 * 16 + nl + lane / GROUP;
-      float x = 0.f;
+      for (int i = 0; i < GB; ++i)
 #pragma unroll
-      for (int w = 0; w < FEW_WAVES; ++w) x += part[w][nl + lane / GROUP][pos];
-      if (v >= V) x = NEG_INF;
-      float m = x;
+        for (int j = 0; j < TURN; ++j)
+          *reinterpret_cast<f32x4*>(&part[wave][j * 16 + row][i * 16 + (lane >> 4) * 4]) = acc[i0 + i][j0 + j];
+      __syncthreads();
+      const int n = j0 * 16 + nl;
+      float x[VPT];
+      for_each_value<VPT>(&part[0][nl][pos], [&](int e, float y) { x[e] = y; });
 #pragma unroll
-      for (int o = GROUP / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-      float e = fast_exp2((x - finite_or_zero(m)) * LOG2E);
+      for (int w = 1; w < FEW_WAVES; ++w) for_each_value<VPT>(&part[w][nl][pos], [&](int e, float y) { x[e] += y; });
+      float m = NEG_INF;
 #pragma unroll
-      for (int o = GROUP / 2; o > 0; o >>= 1) e += __shfl_xor(e, o, 64);
+      for (int e = 0; e < VPT; ++e) {
+        if (g0 + pos + e >= V) x[e] = NEG_INF;
+        m = fmaxf(m, x[e]);
+      }
+#pragma unroll
+      for (int o = 1; o < TPT; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+      const float ms = -finite_or_zero(m) * LOG2E;
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < VPT; ++e) sum += fast_exp2(fmaf(x[e], LOG2E, ms));
+#pragma unroll
+      for (int o = 1; o < TPT; o <<= 1) sum += __shfl_xor(sum, o, 64);
       if (n < N) {
-        z[(int64_t)n * ldz + v] = x;
-        if (pos == 0) stats[(int64_t)n * ld_stats + blockIdx.x] = float2{m, e};
+        float* __restrict__ zn = z + (int64_t)n * ldz + g0 + pos;
+#pragma unroll
+        for (int e = 0; e < VPT; e += VPT < 4 ? VPT : 4) {
+          if constexpr (VPT >= 4) *reinterpret_cast<f32x4*>(zn + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
+          else if constexpr (VPT == 2) *reinterpret_cast<float2*>(zn) = float2{x[0], x[1]};
+          else zn[0] = x[0];
+        }
+        if (pos == 0) stats[(int64_t)n * ld_stats + g0 / GROUP] = float2{m, sum};
       }
     }
   }
 }
 
-// Vocabulary rows per workgroup (16, 32 or 64): as many as leave 512 workgroups, two per CU.
+// Consecutive positions per group (16, 32 or 64): as many as leave 512 workgroups, two per CU.
 inline int few_rows_group(int64_t V) { return V >= 64 * 512 ? 64 : V >= 32 * 512 ? 32 : 16; }
 
+// 17 to 32 rows over a long vocabulary take two groups per workgroup and longer runs (32 rows of 128256 x 4096: 247 us, one group 264); elsewhere
+// the registers that takes cost more than it gives (64 rows 300, two groups 386).
 template <typename T>
 void launch_few_rows(const T* H, const T* W, int N, int d, int V, float* z, int64_t ldz, float2* stats, int64_t ld_stats, hipStream_t st) {
-  const int group = few_rows_group(V), grid = (V + group - 1) / group;
-  auto go = [&](auto kernel) { kernel<<<grid, 64 * FEW_WAVES, 0, st>>>(H, W, N, d, V, z, ldz, stats, ld_stats); };
-  auto by_group = [&](auto nt) {
-    constexpr int NT = decltype(nt)::value;
-    if (group == 64) go(few_rows_kernel<T, 4, NT>);
-    else if (group == 32) go(few_rows_kernel<T, 2, NT>);
-    else go(few_rows_kernel<T, 1, NT>);
+  const int group = few_rows_group(V);
+  auto by = [&](auto mb, auto nt, auto u) {
+    constexpr int MB = decltype(mb)::value, NT = decltype(nt)::value, U = decltype(u)::value;
+    few_rows_kernel<T, MB, NT, U><<<(V + 16 * MB - 1) / (16 * MB), 64 * FEW_WAVES, 0, st>>>(H, W, N, d, V, z, ldz, stats, ld_stats);
   };
-  if (N <= 16) by_group(std::integral_constant<int, 1>{});
-  else if (N <= 32) by_group(std::integral_constant<int, 2>{});
-  else by_group(std::integral_constant<int, 4>{});
+  using std::integral_constant;
+  const integral_constant<int, 2> two{};
+  auto by_group = [&](auto nt) {
+    if (group == 64) by(integral_constant<int, 4>{}, nt, two);
+    else if (group == 32) by(two, nt, two);
+    else by(integral_constant<int, 1>{}, nt, two);
+  };
+  if (N <= 16) by_group(integral_constant<int, 1>{});
+  else if (N <= 32 && V >= 128 * 512) by(integral_constant<int, 8>{}, two, integral_constant<int, 4>{});
+  else if (N <= 32) by_group(two);
+  else by_group(integral_constant<int, 4>{});
 }
 
 }  // namespace flce

@@ -7,7 +7,8 @@ namespace flce {
 constexpr int TOPK_MAX = 256;             // most logits kept of a row
 constexpr int SELECT_THREADS = 256;
 constexpr int SELECT_SORT = 512;          // candidates that are ranked against each other
-constexpr int SELECT_KEYS = 8192;         // group maxima held in LDS
+constexpr int SELECT_GROUPS = 320;        // groups that are looked into: K and a quarter or 16 more
+constexpr int SELECT_HELD = 16;           // group pairs that a thread keeps in registers
 
 // Order of a logit as an unsigned number: NaN above everything, -0 equal to +0.
 __device__ __forceinline__ uint32_t order_key(float x) {
@@ -18,177 +19,264 @@ __device__ __forceinline__ uint32_t order_key(float x) {
 // That of a group: by its maximum, which does not see NaN; its sum does.
 __device__ __forceinline__ uint32_t group_key(float2 s) { return s.y != s.y ? 0xFFFFFFFFu : order_key(s.x); }
 
-struct Threshold {
-  uint32_t key;       // at least `need` keys are >= key, fewer than that are > key
-  int above, equal;   // how many are > key, == key
-};
+__device__ __forceinline__ float value_of(uint32_t key) {
+  return key == 0xFFFFFFFFu ? __builtin_nanf("") : __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
+}
 
-// The need-th largest of n keys (1 <= need <= n) by radix selection, 8 bits at a time from the top: every pass counts the keys
-// that agree with the digits found so far by their next digit.  All threads of a block of SELECT_THREADS call it.
-template <typename GET>
-__device__ __forceinline__ Threshold find_threshold(GET get, int n, int need, int* hist, int* word) {
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  uint32_t prefix = 0;
-  int above = 0, equal = 0;
-#pragma unroll
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    hist[t] = 0;
+// A lower bound of the need-th largest of a set of keys: `above` keys lie above the interval of keys that starts at `low`, `equal` in it,
+// above < need <= above + equal.  The interval is one key where no wider one has above + equal <= limit.
+struct Bound { uint32_t low; int above, equal; };
+
+// By radix selection between the smallest and the largest key, 8 bits at a time from the top: each pass counts the keys of the present
+// interval by their next digit, and ends the search once few enough keys lie above its lower end.  each(f) calls f(key) for every
+// key of the calling thread.  hist: four histograms, zero and a barrier behind them.  Every wavefront reads the histogram for itself, four
+// digits per lane: one barrier per pass.
+template <typename EACH>
+__device__ __forceinline__ Bound find_bound(EACH each, uint32_t kmin, uint32_t kmax, int need, int limit, int (*hist)[256]) {
+  const int lane = threadIdx.x & 63;
+  uint32_t low = kmin;
+  int bits = 32 - __builtin_clz(kmax - kmin | 1u), above = 0, equal = 0;      // digits that are left
+  for (int pass = 0;; ++pass) {
+    const int shift = max(0, bits - 8);
+    const uint32_t span = (bits == 32 ? 0u : 1u << bits) - 1u;                // of the present interval
+    each([&](uint32_t k) {
+      if (k - low <= span && k >= low) atomicAdd(&hist[pass][(k - low) >> shift], 1);
+    });
     __syncthreads();
-    for (int i = t; i < n; i += SELECT_THREADS) {
-      const uint32_t k = get(i);
-      if (shift == 24 || (k ^ prefix) >> (shift + 8) == 0) atomicAdd(&hist[k >> shift & 255], 1);
-    }
-    __syncthreads();
-    // thread t has digit 255 - t: counts of the digits above it by a prefix sum
-    const int c = hist[255 - t];
-    int sum = c;
+    // lane l has the digits 255 - 4 l .. 252 - 4 l
+    const int4 c = *reinterpret_cast<const int4*>(&hist[pass][252 - 4 * lane]);
+    const int mine = c.x + c.y + c.z + c.w;
+    int sum = mine;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
       const int x = __shfl_up(sum, o, 64);
       if (lane >= o) sum += x;
     }
-    if (lane == 63) word[4 + wave] = sum;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < 3; ++w) if (w < wave) sum += word[4 + w];
-    if (above + sum >= need && above + sum - c < need) { word[0] = 255 - t; word[1] = above + sum - c; word[2] = c; }
-    __syncthreads();
-    prefix |= (uint32_t)word[0] << shift;
-    above = word[1];
-    equal = word[2];
+    const int at = __builtin_ctzll(__ballot(above + sum >= need));            // (the last lane's sum reaches it)
+    int before = above + sum - mine, digit = 255 - 4 * lane, count = c.w;
+    if (before + count < need) { before += count; --digit; count = c.z; }
+    if (before + count < need) { before += count; --digit; count = c.y; }
+    if (before + count < need) { before += count; --digit; count = c.x; }
+    above = __builtin_amdgcn_readlane(before, at);
+    equal = __builtin_amdgcn_readlane(count, at);
+    low += (uint32_t)__builtin_amdgcn_readlane(digit, at) << shift;
+    bits = shift;
+    if (shift == 0 || above + equal <= limit) return Bound{low, above, equal};
   }
-  return Threshold{prefix, above, equal};
 }
 
-// The places of the need largest of n keys: those above the threshold and of those equal to it the first ones, into out[].
-// (The order of out is not fixed.)
+// The places of the need largest of n keys (get(i), by threads i, i + 256, ...) in order of their place where they are equal: those above
+// b.low and the first ones equal to it, into out[].  For sets that have more than `limit` keys from a single key on.
 template <typename GET>
-__device__ __forceinline__ void collect(GET get, int n, int need, const Threshold& th, int* out, int* word) {
+__device__ __forceinline__ void collect_first(GET get, int n, int need, const Bound& b, int* out, int* word) {
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  const bool all = th.above + th.equal == need;
-  if (t == 0) word[3] = 0;
+  if (t == 0) word[0] = 0;
   __syncthreads();
-  for (int i = t; i < n; i += SELECT_THREADS) {
-    const uint32_t k = get(i);
-    if (all ? k >= th.key : k > th.key) out[atomicAdd(&word[3], 1)] = i;
-  }
-  if (!all) {
-    int taken = th.above;           // equal ones in order of their place: 256 at a time, wavefront after wavefront
-    for (int i0 = 0; i0 < n && taken < need; i0 += SELECT_THREADS) {
-      const int i = i0 + t;
-      const bool eq = i < n && get(i) == th.key;
-      const uint64_t m = __ballot(eq);
-      __syncthreads();
-      if (lane == 0) word[4 + wave] = __popcll(m);
-      __syncthreads();
-      int at = taken + __popcll(m & ((1ull << lane) - 1));
+  int taken = b.above;
+  for (int i0 = 0; i0 < n; i0 += SELECT_THREADS) {         // 256 at a time, wavefront after wavefront
+    const int i = i0 + t;
+    const uint32_t k = i < n ? get(i) : 0u;
+    const bool eq = i < n && k == b.low;
+    if (i < n && k > b.low) out[atomicAdd(&word[0], 1)] = i;
+    const uint64_t m = __ballot(eq);
+    if (lane == 0) word[4 + wave] = __popcll(m);
+    __syncthreads();
+    int at = taken + __popcll(m & ((1ull << lane) - 1));
 #pragma unroll
-      for (int w = 0; w < SELECT_THREADS / 64; ++w) {
-        if (w < wave) at += word[4 + w];
-        taken += word[4 + w];
-      }
-      if (eq && at < need) out[at] = i;
+    for (int w = 0; w < SELECT_THREADS / 64; ++w) {
+      if (w < wave) at += word[4 + w];
+      taken += word[4 + w];
     }
+    if (eq && at < need) out[at] = i;
+    __syncthreads();
   }
-  __syncthreads();
+}
+
+// out[] gets what f says of the calling thread's items: each(g) calls g(keep, value) the same number of times in all lanes of a wavefront.
+template <typename V, typename EACH>
+__device__ __forceinline__ void append(EACH each, V* out, int room, int* count) {
+  const int lane = threadIdx.x & 63;
+  each([&](bool keep, V value) {
+    const uint64_t m = __ballot(keep);
+    if (m == 0ull) return;
+    int base = 0;
+    if (lane == 0) base = atomicAdd(count, __popcll(m));
+    base = __builtin_amdgcn_readfirstlane(base) + __popcll(m & ((1ull << lane) - 1));
+    if (keep && base < room) out[base] = value;
+  });
 }
 
 // One block per row: the row's K largest logits in order (equal ones by id), their ids, and its log-sum-exp.
-//   1. K groups hold them: the first K by (maximum, position), since an element of another group has K better ones in these.
-//   2. The K-th of those maxima is a lower bound of the K-th logit: of the K groups' elements only the ones that reach it are
-//      candidates, some more than K as a rule.  Where there are more than fit (many equal logits, a band of large ones in
-//      consecutive positions) the K among them are selected first.
+//   1. Any set of groups that has the K with the largest maxima (of equal ones the first) holds them: an element of another group has K
+//      better ones in these.  A bound of the K-th maximum that leaves a few more than K is found first.
+//   2. That bound is a lower bound of the K-th logit too: of those groups' elements only the ones that reach it are candidates, some
+//      more than K as a rule.  Where there are more than fit (many equal logits, a band of large ones in consecutive
+//      positions) the search is repeated on them.
 //   3. A candidate's rank is the number of larger (logit, lower id) pairs.
-// Reads the groups' maxima and K groups of logits; a chain of latencies and barriers, a few us, many rows at a time.
+// Reads the groups' pairs once, where a thread's fit its registers, and some more than K groups of logits; a chain of latencies and seven
+// barriers.
 template <int G>      // positions per group
 __global__ __launch_bounds__(SELECT_THREADS) void select_kernel(const float* __restrict__ z, int64_t ldz, const float2* __restrict__ stats,
                                                                 int64_t ld_stats, int n_groups, int V, int K, float* __restrict__ logits_out,
                                                                 int64_t* __restrict__ ids_out, float* __restrict__ lse_out) {
-  __shared__ uint32_t keys[SELECT_KEYS];
-  __shared__ int hist[SELECT_THREADS], word[8], groups[TOPK_MAX];
-  __shared__ unsigned long long cand[SELECT_SORT];
-  __shared__ float red[2 * SELECT_THREADS / 64];
+  __shared__ __align__(16) int hist[4][256];
+  __shared__ int word[8], groups[SELECT_GROUPS];
+  __shared__ __align__(16) unsigned long long cand[SELECT_SORT];
+  __shared__ float wm[SELECT_THREADS / 64], ws[SELECT_THREADS / 64];
+  __shared__ uint32_t klo[SELECT_THREADS / 64], khi[SELECT_THREADS / 64];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const int64_t row = blockIdx.x;
   z += row * ldz;
   stats += row * ld_stats;
-  const bool in_lds = n_groups <= SELECT_KEYS;
+  const bool held = n_groups <= SELECT_HELD * SELECT_THREADS;
 
-  float m = NEG_INF;
-  for (int g = t; g < n_groups; g += SELECT_THREADS) {
-    const float2 s = stats[g];
+  // Groups' pairs: log-sum-exp, keys and their range.  (A place past the end has key 0, which no logit has.)
+  uint32_t key[SELECT_HELD];
+  float m = NEG_INF, sum = 0.f;
+  uint32_t lo = 0xFFFFFFFFu, hi = 0u;
+  auto take = [&](float2 s) {
     m = fmaxf(m, s.x);
-    if (in_lds) keys[g] = group_key(s);
-  }
+    const uint32_t k = group_key(s);
+    lo = min(lo, k); hi = max(hi, k);
+    return k;
+  };
+  // a group without a finite maximum is relative to 0 (and adds nothing, or +inf)
+  auto add = [&](float2 s) { if (s.y != 0.f) sum += s.y * fast_exp2((finite_or_zero(s.x) - finite_or_zero(m)) * LOG2E); };
+  auto wave_max = [&] {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-  if (lane == 0) red[wave] = m;
-  __syncthreads();
+    for (int o = 32; o > 0; o >>= 1) {
+      m = fmaxf(m, __shfl_xor(m, o, 64));
+      lo = min(lo, (uint32_t)__shfl_xor((int)lo, o, 64));
+      hi = max(hi, (uint32_t)__shfl_xor((int)hi, o, 64));
+    }
+  };
+  if (held) {
+    float2 s[SELECT_HELD];
 #pragma unroll
-  for (int w = 0; w < SELECT_THREADS / 64; ++w) m = fmaxf(m, red[w]);
-  float sum = 0.f;
-  for (int g = t; g < n_groups; g += SELECT_THREADS) {
-    const float2 s = stats[g];
-    // a group without a finite maximum is relative to 0 (and adds nothing, or +inf)
-    if (s.y != 0.f) sum += s.y * fast_exp2((finite_or_zero(s.x) - finite_or_zero(m)) * LOG2E);
+    for (int u = 0; u < SELECT_HELD; ++u)
+      if (u * SELECT_THREADS < n_groups) s[u] = stats[min(t + u * SELECT_THREADS, n_groups - 1)];
+#pragma unroll
+    for (int u = 0; u < SELECT_HELD; ++u) key[u] = t + u * SELECT_THREADS < n_groups ? take(s[u]) : 0u;
+    wave_max();
+#pragma unroll
+    for (int u = 0; u < SELECT_HELD; ++u)
+      if (t + u * SELECT_THREADS < n_groups) add(s[u]);
+  } else {
+    for (int g = t; g < n_groups; g += SELECT_THREADS) take(stats[g]);
+    wave_max();
+    for (int g = t; g < n_groups; g += SELECT_THREADS) add(stats[g]);
   }
   sum = wave_sum(sum);
-  if (lane == 0) red[SELECT_THREADS / 64 + wave] = sum;
-  __syncthreads();
-  if (t == 0) {
-    float a = 0.f;
 #pragma unroll
-    for (int w = 0; w < SELECT_THREADS / 64; ++w) a += red[SELECT_THREADS / 64 + w];
-    lse_out[row] = finite_or_zero(m) + logf(a);
+  for (int p = 0; p < 4; ++p) hist[p][t] = 0;
+  if (lane == 0) { wm[wave] = m; ws[wave] = sum; klo[wave] = lo; khi[wave] = hi; }
+  if (t < 2) word[t] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < SELECT_THREADS / 64; ++w) { lo = min(lo, klo[w]); hi = max(hi, khi[w]); }
+  if (t == 0) {
+    float M = NEG_INF, a = 0.f;
+#pragma unroll
+    for (int w = 0; w < SELECT_THREADS / 64; ++w) M = fmaxf(M, wm[w]);
+#pragma unroll
+    for (int w = 0; w < SELECT_THREADS / 64; ++w)
+      if (ws[w] != 0.f) a += ws[w] * fast_exp2((finite_or_zero(wm[w]) - finite_or_zero(M)) * LOG2E);
+    lse_out[row] = finite_or_zero(M) + logf(a);
   }
 
-  auto key_of_group = [&](int g) { return in_lds ? keys[g] : group_key(stats[g]); };
-  const int kg = min(K, n_groups);
-  Threshold th{0u, 0, n_groups};
-  if (kg < n_groups) th = find_threshold(key_of_group, n_groups, kg, hist, word);
-  collect(key_of_group, n_groups, kg, th, groups, word);
+  auto group_keys = [&](auto f) {
+    if (held) {
+#pragma unroll
+      for (int u = 0; u < SELECT_HELD; ++u)
+        if (t + u * SELECT_THREADS < n_groups) f(key[u]);
+    } else {
+      for (int g = t; g < n_groups; g += SELECT_THREADS) f(group_key(stats[g]));
+    }
+  };
+  const int want = min(K, n_groups);
+  Bound b{0u, 0, n_groups};
+  if (n_groups > want) b = find_bound(group_keys, lo, hi, want, want + max(16, want / 4), hist);
+  int n_held = b.above + b.equal;
+  if (n_held <= SELECT_GROUPS) {
+    append<int>([&](auto f) {
+      if (held) {
+#pragma unroll
+        for (int u = 0; u < SELECT_HELD; ++u)
+          if (u * SELECT_THREADS < n_groups) f(t + u * SELECT_THREADS < n_groups && key[u] >= b.low, t + u * SELECT_THREADS);
+      } else {
+        for (int g0 = 0; g0 < n_groups; g0 += SELECT_THREADS) f(g0 + t < n_groups && group_key(stats[g0 + t]) >= b.low, g0 + t);
+      }
+    }, groups, SELECT_GROUPS, &word[0]);
+    __syncthreads();
+  } else {
+    n_held = want;
+    collect_first([&](int g) { return group_key(stats[g]); }, n_groups, want, b, groups, word);
+  }
 
-  const int n = kg * G;
+  const int n = n_held * G;
   auto place = [&](int i) { return groups[i / G] * G + i % G; };
   // a position past the vocabulary's end lies below everything, -inf included (whose key is not 0)
   auto key_of = [&](int i) { const int v = place(i); return v < V ? order_key(z[v]) : 0u; };
-  if (t == 0) word[3] = 0;
-  __syncthreads();
-  const uint32_t low = kg == K ? max(th.key, 1u) : 1u;     // fewer groups than K: every element is a candidate
-  for (int i = t; i < n; i += SELECT_THREADS) {
-    const uint32_t k = key_of(i);
-    if (k >= low) {
-      const int at = atomicAdd(&word[3], 1);
-      if (at < SELECT_SORT) cand[at] = (unsigned long long)k << 32 | (uint32_t)~place(i);
+  const uint32_t low = n_groups >= K ? max(b.low, 1u) : 1u;     // fewer groups than K: every element is a candidate
+  append<unsigned long long>([&](auto f) {
+    constexpr int U = 4;
+    for (int i0 = 0; i0 < n; i0 += U * SELECT_THREADS) {
+      uint32_t k[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) k[u] = key_of(min(i0 + u * SELECT_THREADS + t, n - 1));
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = i0 + u * SELECT_THREADS + t;
+        f(i < n && k[u] >= low, (unsigned long long)k[u] << 32 | (uint32_t)~place(min(i, n - 1)));
+      }
     }
-  }
+  }, cand, SELECT_SORT, &word[1]);
   __syncthreads();
-  int count = word[3];
-  __syncthreads();
+  int count = word[1];
   if (count > SELECT_SORT) {
     // in order of their ids, so that the first of equal ones are the lowest
-    int rank = 0, mine = t < kg ? groups[t] : 0;
-    for (int g = 0; g < kg; ++g) rank += groups[g] < mine;
     __syncthreads();
-    if (t < kg) groups[rank] = mine;
+    int rank[2] = {0, 0}, mine[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      mine[u] = t + u * SELECT_THREADS < n_held ? groups[t + u * SELECT_THREADS] : 0;
+      for (int g = 0; g < n_held; ++g) rank[u] += groups[g] < mine[u];
+    }
+#pragma unroll
+    for (int p = 0; p < 4; ++p) hist[p][t] = 0;
+    if (t == 0) word[1] = 0;
     __syncthreads();
-    const Threshold te = find_threshold(key_of, n, K, hist, word);
-    int* chosen = reinterpret_cast<int*>(cand);            // K <= 256 places, then their pairs in the same memory
-    collect(key_of, n, K, te, chosen, word);
-    const int i = t < K ? chosen[t] : 0;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      if (t + u * SELECT_THREADS < n_held) groups[rank[u]] = mine[u];
     __syncthreads();
-    if (t < K) cand[t] = (unsigned long long)key_of(i) << 32 | (uint32_t)~place(i);
+    const Bound e = find_bound([&](auto f) { for (int i = t; i < n; i += SELECT_THREADS) f(key_of(i)); }, 0u, 0xFFFFFFFFu, K, SELECT_SORT, hist);
+    count = e.above + e.equal;
+    if (count <= SELECT_SORT) {
+      append<unsigned long long>([&](auto f) {
+        for (int i0 = 0; i0 < n; i0 += SELECT_THREADS) {
+          const int i = min(i0 + t, n - 1);
+          const uint32_t k = key_of(i);
+          f(i0 + t < n && k >= e.low, (unsigned long long)k << 32 | (uint32_t)~place(i));
+        }
+      }, cand, SELECT_SORT, &word[1]);
+    } else {
+      int* chosen = reinterpret_cast<int*>(cand);          // K <= 256 places, then their pairs in the same memory
+      collect_first(key_of, n, K, e, chosen, word);
+      const int i = t < K ? chosen[t] : 0;
+      __syncthreads();
+      if (t < K) cand[t] = (unsigned long long)key_of(i) << 32 | (uint32_t)~place(i);
+      count = K;
+    }
     __syncthreads();
-    count = K;
   }
   for (int i = t; i < count; i += SELECT_THREADS) {
     const unsigned long long c = cand[i];
     int rank = 0;
     for (int o = 0; o < count; ++o) rank += cand[o] > c;
     if (rank < K) {
-      const int v = (int)~(uint32_t)c;
-      logits_out[row * K + rank] = z[v];
-      ids_out[row * K + rank] = v;
+      logits_out[row * K + rank] = value_of((uint32_t)(c >> 32));
+      ids_out[row * K + rank] = (int)~(uint32_t)c;
     }
   }
 }
