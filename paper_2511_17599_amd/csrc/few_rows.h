@@ -4,7 +4,6 @@
 
 namespace flce {
 
-constexpr int FEW_ROWS = 64;          // rows up to which this kernel is used
 constexpr int FEW_WAVES = 4;
 
 // 64 bytes of K of 16 rows per step and fragment: lane l holds 16 bytes of row l % 16, from byte 16 (l / 16) on.
@@ -41,20 +40,20 @@ __device__ __forceinline__ void for_each_value(const float* p, F f) {
 // One workgroup: 16 MB vocabulary rows by 16 NT token rows.  Its four wavefronts take U consecutive K steps (64 U bytes of a row of W) in
 // turn, and their sums are added in wavefront order through LDS.
 // W goes from memory to the matrix instruction's registers without a stop in LDS: no element of it is used twice by a wavefront.
-// Bound by the read of W (128256 x 4096 in bf16, this kernel and the selection: 1 row 217 us, 32 rows 247, 64 rows 300); H (N d elements,
-// from the L2) is read once per workgroup.  Tried and no faster: a wavefront per group with H shared through LDS or the L1 (32 rows 251 to
+// Bound by the read of W (128256 x 4096 in bf16: 1 row 200 us or 5.2 TB/s, 32 rows 227); H (N d elements, from the L2) is read once per
+// workgroup.  Tried and no faster: a wavefront per group with H shared through LDS or the L1 (32 rows 251 to
 // 283), the next run's loads issued ahead of the products (registers for them cost more wavefronts than they gain), loads of W
 // that pass the caches (291).
 template <typename T, int MB, int NT, int U>
 __global__ __launch_bounds__(64 * FEW_WAVES) void few_rows_kernel(const T* __restrict__ H, const T* __restrict__ W, int N, int d, int V,
                                                                   float* __restrict__ z, int64_t ldz, float2* __restrict__ stats,
-                                                                  int64_t ld_stats) {
+                                                                  int64_t ld_stats, ZeroWords zero) {
   constexpr int VEC = 16 / (int)sizeof(T), STEP = 4 * VEC, GB = MB < 4 ? MB : 4, GROUP = 16 * GB, LD = GROUP + 4;
-  constexpr int TURN = GB * NT >= 16 ? NT / 2 : NT;       // blocks of tokens that go through LDS at a time (35 KiB at most)
-  __shared__ __align__(16) float part[FEW_WAVES][16 * TURN][LD];
+  __shared__ __align__(16) float part[FEW_WAVES][16 * NT][LD];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int row = lane & 15, k0 = (lane >> 4) * VEC;
   const int v0 = blockIdx.x * (16 * MB);
+  zero.by_first_block();
   const T* wp[MB];
   const T* hp[NT];
 #pragma unroll
@@ -97,81 +96,83 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void few_rows_kernel(const T* __res
       for (int j = 0; j < NT; ++j) FewMma<T>::run(a[i], b[j], acc[i][j]);
   }
 
-  // One group of the workgroup's and TURN blocks of tokens at a time: TPT neighbouring lanes have a token, VPT positions each.
-  constexpr int TPT = 64 * FEW_WAVES / (16 * TURN), VPT = GROUP / TPT;
+  // One group of the workgroup's at a time: TPT neighbouring lanes have a token, VPT positions each.
+  constexpr int TPT = 64 * FEW_WAVES / (16 * NT), VPT = GROUP / TPT;
   static_assert(VPT >= 1 && (VPT & (VPT - 1)) == 0, "lanes and positions of a token");
-  const int nl = threadIdx.x / TPT, pos = threadIdx.x % TPT * VPT;
+  const int n = threadIdx.x / TPT, pos = threadIdx.x % TPT * VPT;
 #pragma unroll
   for (int i0 = 0; i0 < MB; i0 += GB) {
     const int g0 = v0 + i0 * 16;
     if (g0 >= V) break;
+    if (i0 > 0) __syncthreads();
+    // block (i, j): element r of a lane is vocabulary row 4 (l / 16) + r, token l % 16
 #pragma unroll
-    for (int j0 = 0; j0 < NT; j0 += TURN) {
-      if (j0 * 16 >= N) break;
-      if (i0 + j0 > 0) __syncthreads();
-      // block (i, j): element r of a lane is vocabulary row 4 (l / 16) + r, token l % 16
+    for (int i = 0; i < GB; ++i)
 #pragma unroll
-      for (int i = 0; i < GB; ++i)
+      for (int j = 0; j < NT; ++j)
+        *reinterpret_cast<f32x4*>(&part[wave][j * 16 + row][i * 16 + (lane >> 4) * 4]) = acc[i0 + i][j];
+    __syncthreads();
+    float x[VPT];
+    for_each_value<VPT>(&part[0][n][pos], [&](int e, float y) { x[e] = y; });
 #pragma unroll
-        for (int j = 0; j < TURN; ++j)
-          *reinterpret_cast<f32x4*>(&part[wave][j * 16 + row][i * 16 + (lane >> 4) * 4]) = acc[i0 + i][j0 + j];
-      __syncthreads();
-      const int n = j0 * 16 + nl;
-      float x[VPT];
-      for_each_value<VPT>(&part[0][nl][pos], [&](int e, float y) { x[e] = y; });
+    for (int w = 1; w < FEW_WAVES; ++w) for_each_value<VPT>(&part[w][n][pos], [&](int e, float y) { x[e] += y; });
+    float m = NEG_INF;
 #pragma unroll
-      for (int w = 1; w < FEW_WAVES; ++w) for_each_value<VPT>(&part[w][nl][pos], [&](int e, float y) { x[e] += y; });
-      float m = NEG_INF;
+    for (int e = 0; e < VPT; ++e) {
+      if (g0 + pos + e >= V) x[e] = NEG_INF;
+      m = fmaxf(m, x[e]);
+    }
 #pragma unroll
-      for (int e = 0; e < VPT; ++e) {
-        if (g0 + pos + e >= V) x[e] = NEG_INF;
-        m = fmaxf(m, x[e]);
+    for (int o = 1; o < TPT; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+    const float ms = -finite_or_zero(m) * LOG2E;
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < VPT; ++e) sum += fast_exp2(fmaf(x[e], LOG2E, ms));
+#pragma unroll
+    for (int o = 1; o < TPT; o <<= 1) sum += __shfl_xor(sum, o, 64);
+    if (n < N) {
+      float* __restrict__ zn = z + (int64_t)n * ldz + g0 + pos;
+#pragma unroll
+      for (int e = 0; e < VPT; e += VPT < 4 ? VPT : 4) {
+        if constexpr (VPT >= 4) *reinterpret_cast<f32x4*>(zn + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
+        else if constexpr (VPT == 2) *reinterpret_cast<float2*>(zn) = float2{x[0], x[1]};
+        else zn[0] = x[0];
       }
-#pragma unroll
-      for (int o = 1; o < TPT; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-      const float ms = -finite_or_zero(m) * LOG2E;
-      float sum = 0.f;
-#pragma unroll
-      for (int e = 0; e < VPT; ++e) sum += fast_exp2(fmaf(x[e], LOG2E, ms));
-#pragma unroll
-      for (int o = 1; o < TPT; o <<= 1) sum += __shfl_xor(sum, o, 64);
-      if (n < N) {
-        float* __restrict__ zn = z + (int64_t)n * ldz + g0 + pos;
-#pragma unroll
-        for (int e = 0; e < VPT; e += VPT < 4 ? VPT : 4) {
-          if constexpr (VPT >= 4) *reinterpret_cast<f32x4*>(zn + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
-          else if constexpr (VPT == 2) *reinterpret_cast<float2*>(zn) = float2{x[0], x[1]};
-          else zn[0] = x[0];
-        }
-        if (pos == 0) stats[(int64_t)n * ld_stats + g0 / GROUP] = float2{m, sum};
-      }
+      if (pos == 0) stats[(int64_t)n * ld_stats + g0 / GROUP] = float2{m, sum};
     }
   }
 }
 
 // Consecutive positions per group (16, 32 or 64): as many as leave 512 workgroups, two per CU.
 inline int few_rows_group(int64_t V) { return V >= 64 * 512 ? 64 : V >= 32 * 512 ? 32 : 16; }
+// Whether this kernel takes a call (otherwise the tiles of the forward's loop do).  Both, us, selection included: bf16 128256 x 4096
+// 4 rows 208 / 237, 32 rows 233 / 243, 64 rows 288 / 251; 32000 x 1024 32 rows 26.9 / 27.0, 64 rows 36.7 / 27.3; 8192 x 4096 64 rows
+// 46.7 / 53.7; fp32 50257 x 768 4 rows 43 / 86, 32 rows 61 / 87, 64 rows 91 / 87.
+inline bool few_rows_ok(int64_t N, int64_t V) { return N <= 32 || (N <= 64 && few_rows_group(V) == 16); }
 
 // 17 to 32 rows over a long vocabulary take two groups per workgroup and longer runs (32 rows of 128256 x 4096: 247 us, one group 264); elsewhere
-// the registers that takes cost more than it gives (64 rows 300, two groups 386).
+// the registers that takes cost more than it gives (1 row 217, two groups 221).
 template <typename T>
-void launch_few_rows(const T* H, const T* W, int N, int d, int V, float* z, int64_t ldz, float2* stats, int64_t ld_stats, hipStream_t st) {
+void launch_few_rows(const T* H, const T* W, int N, int d, int V, float* z, int64_t ldz, float2* stats, int64_t ld_stats, ZeroWords zero,
+                     hipStream_t st) {
   const int group = few_rows_group(V);
   auto by = [&](auto mb, auto nt, auto u) {
     constexpr int MB = decltype(mb)::value, NT = decltype(nt)::value, U = decltype(u)::value;
-    few_rows_kernel<T, MB, NT, U><<<(V + 16 * MB - 1) / (16 * MB), 64 * FEW_WAVES, 0, st>>>(H, W, N, d, V, z, ldz, stats, ld_stats);
+    few_rows_kernel<T, MB, NT, U><<<(V + 16 * MB - 1) / (16 * MB), 64 * FEW_WAVES, 0, st>>>(H, W, N, d, V, z, ldz, stats, ld_stats, zero);
   };
   using std::integral_constant;
+  const integral_constant<int, 1> one{};
   const integral_constant<int, 2> two{};
+  const integral_constant<int, 4> four{};
   auto by_group = [&](auto nt) {
-    if (group == 64) by(integral_constant<int, 4>{}, nt, two);
+    if (group == 64) by(four, nt, two);
     else if (group == 32) by(two, nt, two);
-    else by(integral_constant<int, 1>{}, nt, two);
+    else by(one, nt, two);
   };
-  if (N <= 16) by_group(integral_constant<int, 1>{});
-  else if (N <= 32 && V >= 128 * 512) by(integral_constant<int, 8>{}, two, integral_constant<int, 4>{});
-  else if (N <= 32) by_group(two);
-  else by_group(integral_constant<int, 4>{});
+  if (N <= 16) by_group(one);
+  else if (N > 32) by(one, four, two);
+  else if (V >= 128 * 512) by(integral_constant<int, 8>{}, two, four);
+  else by_group(two);
 }
 
 }  // namespace flce

@@ -6,12 +6,22 @@
 
 namespace flce {
 
+// Words that a later kernel on the stream counts in.
+struct ZeroWords {
+  uint32_t* word; int n;
+  __device__ __forceinline__ void by_first_block() const {
+    if (blockIdx.x == 0)
+      for (int i = threadIdx.x; i < n; i += blockDim.x) word[i] = 0u;
+  }
+};
+
 template <typename T>
 struct LogitArgs {
   const T* H; const T* HT; const T* W;
   int N, d, V, nt0, n_nt, n_vt;         // row tiles nt0 .. nt0 + n_nt - 1 by all vocabulary tiles
   float2* stats; int64_t ld_stats;      // [row - first row][group]: (max z, sum exp(z - max))
   float* z; int64_t ldz;                // [row - first row][position], up to whole tiles
+  ZeroWords zero;
 };
 
 // The lanes of a wavefront that share a token column (every sixteenth or every thirty-second): their maximum, their sum, in a fixed
@@ -38,6 +48,7 @@ __global__ __launch_bounds__(L::THREADS, L::MIN_WAVES) void logit_tiles_kernel(L
   extern __shared__ __align__(16) char lds[];
   constexpr int COLS = L::ROWS == 64 ? 16 : 32;         // token columns of a block
   const int lane = threadIdx.x & 63;
+  a.zero.by_first_block();
   const int total = a.n_nt * a.n_vt;
   const int64_t ld_bytes = (int64_t)a.d * sizeof(T);
   int t = blockIdx.x;

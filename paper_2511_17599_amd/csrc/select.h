@@ -106,6 +106,89 @@ __device__ __forceinline__ void append(EACH each, V* out, int room, int* count) 
   });
 }
 
+// A beam search's step on top of the selection: the rows of a search hand their candidates over, and the block that does so last ranks
+// them all (a launch of its own took 4 to 5 us).
+struct BeamStep {
+  const float* scores; const uint8_t* finished;
+  int64_t row0; int beams, n_out;
+  int64_t eos_id, pad_id;
+  float* scores_out; int64_t* tokens_out; int64_t* parents_out; uint8_t* finished_out;
+  uint32_t* arrived;                // [search], zero
+  unsigned long long* cand;         // [row][K]: (key, ~id) in order
+  float* lse;                       // [row]
+  __device__ __forceinline__ bool done(int64_t row) const { return finished && finished[row]; }
+};
+
+// Scores of a beam's candidates are in order as its logits are; a finished beam is its own one candidate.  A candidate's rank is its
+// place in its own beam's list plus the number of candidates of the other beams that come before it (a binary search in each list):
+// larger score first, equal ones by beam.  key: [beams][K], len: [beams] in LDS.
+__device__ __forceinline__ void rank_beams(const BeamStep& s, int K, int64_t search, uint32_t* key, int* len) {
+  const int64_t row0 = search * s.beams;
+  auto pair = [&](int i) {          // (written by other blocks of this launch: read past this XCD's own caches)
+    return __hip_atomic_load(s.cand + row0 * K + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  };
+  for (int i = threadIdx.x; i < s.beams * K; i += SELECT_THREADS) {
+    const int j = i / K;
+    float x = s.scores[row0 + j];
+    // (NaN and +inf stay what they are, so that a beam's scores are in order whatever its logits)
+    if (!s.done(row0 + j) && x < __builtin_inff())
+      x += value_of((uint32_t)(pair(i) >> 32)) - __hip_atomic_load(s.lse + row0 + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    key[i] = order_key(x);
+  }
+  for (int j = threadIdx.x; j < s.beams; j += SELECT_THREADS) len[j] = s.done(row0 + j) ? 1 : K;
+  __syncthreads();
+  int total = 0;
+  for (int j = 0; j < s.beams; ++j) total += len[j];
+  for (int i = threadIdx.x; i < s.beams * K; i += SELECT_THREADS) {
+    const int j = i / K, k = i % K;
+    if (k >= len[j]) continue;
+    const uint32_t mine = key[i];
+    int rank = k;
+    for (int o = 0; o < s.beams && rank < s.n_out; ++o) {
+      if (o == j) continue;
+      int lo = 0, hi = len[o];         // how many of beam o come first: larger ones, of a lower beam equal ones too
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        const uint32_t x = key[o * K + mid];
+        if (x > mine || (x == mine && o < j)) lo = mid + 1; else hi = mid;
+      }
+      rank += lo;
+    }
+    if (rank >= s.n_out) continue;
+    const bool done = s.done(row0 + j);
+    const int64_t token = done ? s.pad_id : (int64_t)(int)~(uint32_t)pair(i);
+    const int64_t at = search * s.n_out + rank;
+    s.scores_out[at] = value_of(mine);
+    s.tokens_out[at] = token;
+    s.parents_out[at] = j;
+    s.finished_out[at] = done || token == s.eos_id;
+  }
+  // fewer candidates than places: dead results
+  for (int r = total + threadIdx.x; r < s.n_out; r += SELECT_THREADS) {
+    const int64_t at = search * s.n_out + r;
+    s.scores_out[at] = NEG_INF;
+    s.tokens_out[at] = s.pad_id;
+    s.parents_out[at] = 0;
+    s.finished_out[at] = 1;
+  }
+}
+
+// The end of a row's block: what it has stored has reached the point the other XCDs read from before it counts as arrived.
+__device__ __forceinline__ void arrive(const BeamStep& s, int K, int64_t row) {
+  extern __shared__ __align__(16) char dyn[];
+  __shared__ int last;
+  const int64_t search = (s.row0 + row) / s.beams;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0)
+    last = __hip_atomic_fetch_add(s.arrived + search, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)s.beams - 1;
+  __syncthreads();
+  if (last) {
+    uint32_t* key = reinterpret_cast<uint32_t*>(dyn);
+    rank_beams(s, K, search, key, reinterpret_cast<int*>(key + s.beams * K));
+  }
+}
+
 // One block per row: the row's K largest logits in order (equal ones by id), their ids, and its log-sum-exp.
 //   1. Any set of groups that has the K with the largest maxima (of equal ones the first) holds them: an element of another group has K
 //      better ones in these.  A bound of the K-th maximum that leaves a few more than K is found first.
@@ -115,10 +198,12 @@ __device__ __forceinline__ void append(EACH each, V* out, int room, int* count) 
 //   3. A candidate's rank is the number of larger (logit, lower id) pairs.
 // Reads the groups' pairs once, where a thread's fit its registers, and some more than K groups of logits; a chain of latencies and seven
 // barriers.
-template <int G>      // positions per group
-__global__ __launch_bounds__(SELECT_THREADS) void select_kernel(const float* __restrict__ z, int64_t ldz, const float2* __restrict__ stats,
-                                                                int64_t ld_stats, int n_groups, int V, int K, float* __restrict__ logits_out,
-                                                                int64_t* __restrict__ ids_out, float* __restrict__ lse_out) {
+// OUT: Largest, or BeamStep with beams (K + 1) words of dynamic LDS.
+struct Largest { float* logits; int64_t* ids; float* lse; };      // [row][K], [row][K], [row] from the launch's first row on
+template <int G, typename OUT>      // positions per group
+__device__ __forceinline__ void select_row(const float* __restrict__ z, int64_t ldz, const float2* __restrict__ stats, int64_t ld_stats,
+                                           int n_groups, int V, int K, const OUT& out) {
+  constexpr bool BEAM = std::is_same<OUT, BeamStep>::value;
   __shared__ __align__(16) int hist[4][256];
   __shared__ int word[8], groups[SELECT_GROUPS];
   __shared__ __align__(16) unsigned long long cand[SELECT_SORT];
@@ -160,7 +245,7 @@ __global__ __launch_bounds__(SELECT_THREADS) void select_kernel(const float* __r
     wave_max();
 #pragma unroll
     for (int u = 0; u < SELECT_HELD; ++u)
-      if (t + u * SELECT_THREADS < n_groups) add(s[u]);
+      if (key[u] != 0u) add(s[u]);
   } else {
     for (int g = t; g < n_groups; g += SELECT_THREADS) take(stats[g]);
     wave_max();
@@ -181,14 +266,16 @@ __global__ __launch_bounds__(SELECT_THREADS) void select_kernel(const float* __r
 #pragma unroll
     for (int w = 0; w < SELECT_THREADS / 64; ++w)
       if (ws[w] != 0.f) a += ws[w] * fast_exp2((finite_or_zero(wm[w]) - finite_or_zero(M)) * LOG2E);
-    lse_out[row] = finite_or_zero(M) + logf(a);
+    const float lse = finite_or_zero(M) + logf(a);
+    if constexpr (BEAM) __hip_atomic_store(out.lse + out.row0 + row, lse, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    else out.lse[row] = lse;
   }
 
   auto group_keys = [&](auto f) {
     if (held) {
 #pragma unroll
       for (int u = 0; u < SELECT_HELD; ++u)
-        if (t + u * SELECT_THREADS < n_groups) f(key[u]);
+        if (key[u] != 0u) f(key[u]);
     } else {
       for (int g = t; g < n_groups; g += SELECT_THREADS) f(group_key(stats[g]));
     }
@@ -202,7 +289,7 @@ __global__ __launch_bounds__(SELECT_THREADS) void select_kernel(const float* __r
       if (held) {
 #pragma unroll
         for (int u = 0; u < SELECT_HELD; ++u)
-          if (u * SELECT_THREADS < n_groups) f(t + u * SELECT_THREADS < n_groups && key[u] >= b.low, t + u * SELECT_THREADS);
+          if (u * SELECT_THREADS < n_groups) f(key[u] >= max(b.low, 1u), t + u * SELECT_THREADS);
       } else {
         for (int g0 = 0; g0 < n_groups; g0 += SELECT_THREADS) f(g0 + t < n_groups && group_key(stats[g0 + t]) >= b.low, g0 + t);
       }
@@ -275,67 +362,24 @@ __global__ __launch_bounds__(SELECT_THREADS) void select_kernel(const float* __r
     int rank = 0;
     for (int o = 0; o < count; ++o) rank += cand[o] > c;
     if (rank < K) {
-      logits_out[row * K + rank] = value_of((uint32_t)(c >> 32));
-      ids_out[row * K + rank] = (int)~(uint32_t)c;
+      if constexpr (BEAM) {
+        __hip_atomic_store(out.cand + (out.row0 + row) * K + rank, c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      } else {
+        out.logits[row * K + rank] = value_of((uint32_t)(c >> 32));
+        out.ids[row * K + rank] = (int)~(uint32_t)c;
+      }
     }
   }
 }
 
-// A beam's candidates in order: the rows' largest logits as scores; a finished beam's is the one that it is.
-// One block per batch element.  A candidate's rank is its place in its own beam's list plus the number of candidates of the
-// other beams that come before it (a binary search in each list, which is in order): larger score first, equal ones by beam.
-__global__ __launch_bounds__(SELECT_THREADS) void beam_select_kernel(const float* __restrict__ logits, const int64_t* __restrict__ ids,
-                                                                     const float* __restrict__ lse, const float* __restrict__ scores,
-                                                                     const uint8_t* __restrict__ finished, int beams, int K, int n_out,
-                                                                     int64_t eos_id, int64_t pad_id, float* __restrict__ scores_out,
-                                                                     int64_t* __restrict__ tokens_out, int64_t* __restrict__ parents_out,
-                                                                     uint8_t* __restrict__ finished_out) {
-  extern __shared__ __align__(16) char dyn[];
-  uint32_t* key = reinterpret_cast<uint32_t*>(dyn);        // [beams][K]
-  int* len = reinterpret_cast<int*>(key + beams * K);      // [beams]
-  const int b = blockIdx.x;
-  const int64_t row0 = (int64_t)b * beams;
-  auto score = [&](int j, int k) {
-    const float s = scores[row0 + j];
-    // (NaN and +inf stay what they are, so that a beam's scores are in order whatever its logits)
-    return (finished && finished[row0 + j]) || !(s < __builtin_inff()) ? s : s + (logits[(row0 + j) * K + k] - lse[row0 + j]);
-  };
-  for (int i = threadIdx.x; i < beams * K; i += SELECT_THREADS) key[i] = order_key(score(i / K, i % K));
-  for (int j = threadIdx.x; j < beams; j += SELECT_THREADS) len[j] = finished && finished[row0 + j] ? 1 : K;
-  __syncthreads();
-  int total = 0;
-  for (int j = 0; j < beams; ++j) total += len[j];
-  for (int i = threadIdx.x; i < beams * K; i += SELECT_THREADS) {
-    const int j = i / K, k = i % K;
-    if (k >= len[j]) continue;
-    const uint32_t mine = key[i];
-    int rank = k;
-    for (int o = 0; o < beams && rank < n_out; ++o) {
-      if (o == j) continue;
-      int lo = 0, hi = len[o];         // how many of beam o come first: larger ones, of a lower beam equal ones too
-      while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        const uint32_t x = key[o * K + mid];
-        if (x > mine || (x == mine && o < j)) lo = mid + 1; else hi = mid;
-      }
-      rank += lo;
-    }
-    if (rank >= n_out) continue;
-    const bool done = finished && finished[row0 + j];
-    const int64_t token = done ? pad_id : ids[(row0 + j) * K + k];
-    const int64_t at = (int64_t)b * n_out + rank;
-    scores_out[at] = score(j, k);
-    tokens_out[at] = token;
-    parents_out[at] = j;
-    finished_out[at] = done || token == eos_id;
-  }
-  // fewer candidates than places: dead results
-  for (int r = total + threadIdx.x; r < n_out; r += SELECT_THREADS) {
-    const int64_t at = (int64_t)b * n_out + r;
-    scores_out[at] = NEG_INF;
-    tokens_out[at] = pad_id;
-    parents_out[at] = 0;
-    finished_out[at] = 1;
+template <int G, typename OUT>
+__global__ __launch_bounds__(SELECT_THREADS) void select_kernel(const float* __restrict__ z, int64_t ldz, const float2* __restrict__ stats,
+                                                                int64_t ld_stats, int n_groups, int V, int K, OUT out) {
+  if constexpr (std::is_same<OUT, BeamStep>::value) {
+    if (!out.done(out.row0 + blockIdx.x)) select_row<G>(z, ldz, stats, ld_stats, n_groups, V, K, out);
+    arrive(out, K, blockIdx.x);
+  } else {
+    select_row<G>(z, ldz, stats, ld_stats, n_groups, V, K, out);
   }
 }
 

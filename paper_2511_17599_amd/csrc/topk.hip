@@ -24,7 +24,7 @@ bool make_topk_plan(int64_t N, int64_t d, int64_t V, int64_t K, flce_dtype dt, T
   if (!make_plan(PLAN_FORWARD, N, d, V, dt, t.p)) return false;
   if (K < 1 || K > TOPK_MAX || K > V || V > TOPK_MAX_V) return false;
   const Plan& p = t.p;
-  t.few = N <= FEW_ROWS;
+  t.few = few_rows_ok(N, V);
   int64_t o = 0;
   if (t.few) {
     t.group = few_rows_group(V);
@@ -48,20 +48,19 @@ bool make_topk_plan(int64_t N, int64_t d, int64_t V, int64_t K, flce_dtype dt, T
   return true;
 }
 
-void launch_select(const TopkPlan& t, int64_t rows, int64_t row0, int K, char* ws, float* logits, int64_t* ids, float* lse, hipStream_t st) {
+// `out` says where the rows' selections go: out(row0) for a launch of rows from row0 on; `lds` is its dynamic LDS.
+template <typename OUT>
+void launch_select(const TopkPlan& t, int64_t rows, int K, char* ws, const OUT& out, size_t lds, hipStream_t st) {
   const float* z = reinterpret_cast<const float*>(ws + t.off_z);
   const float2* stats = reinterpret_cast<const float2*>(ws + t.off_stats);
-  auto go = [&](auto kernel) {
-    kernel<<<(unsigned)rows, SELECT_THREADS, 0, st>>>(z, t.ldz, stats, t.ld_stats, t.n_groups, (int)t.p.V, K, logits + row0 * K,
-                                                      ids + row0 * K, lse + row0);
-  };
-  if (t.group == 64) go(select_kernel<64>);
-  else if (t.group == 32) go(select_kernel<32>);
-  else go(select_kernel<16>);
+  auto go = [&](auto kernel) { kernel<<<(unsigned)rows, SELECT_THREADS, lds, st>>>(z, t.ldz, stats, t.ld_stats, t.n_groups, (int)t.p.V, K, out); };
+  if (t.group == 64) go(select_kernel<64, OUT>);
+  else if (t.group == 32) go(select_kernel<32, OUT>);
+  else go(select_kernel<16, OUT>);
 }
 
-flce_status run_topk(const TopkPlan& t, const void* H, const void* W, int K, char* ws, float* logits, int64_t* ids, float* lse,
-                     hipStream_t st) {
+template <typename F>
+flce_status run_topk(const TopkPlan& t, const void* H, const void* W, int K, char* ws, F out, size_t lds, ZeroWords zero, hipStream_t st) {
   const Plan& p = t.p;
   const int N = (int)p.N, d = (int)p.d, V = (int)p.V;
   float* z = reinterpret_cast<float*>(ws + t.off_z);
@@ -69,11 +68,13 @@ flce_status run_topk(const TopkPlan& t, const void* H, const void* W, int K, cha
   if (t.few) {
     {
       ProfScope ps(FLCE_PROF_FWD_TILES, st);
-      if (p.esize == 2) launch_few_rows(static_cast<const bf16_t*>(H), static_cast<const bf16_t*>(W), N, d, V, z, t.ldz, stats, t.ld_stats, st);
-      else launch_few_rows(static_cast<const float*>(H), static_cast<const float*>(W), N, d, V, z, t.ldz, stats, t.ld_stats, st);
+      if (p.esize == 2)
+        launch_few_rows(static_cast<const bf16_t*>(H), static_cast<const bf16_t*>(W), N, d, V, z, t.ldz, stats, t.ld_stats, zero, st);
+      else
+        launch_few_rows(static_cast<const float*>(H), static_cast<const float*>(W), N, d, V, z, t.ldz, stats, t.ld_stats, zero, st);
     }
     ProfScope ps(FLCE_PROF_FWD_EPILOGUE, st);
-    launch_select(t, N, 0, K, ws, logits, ids, lse, st);
+    launch_select(t, N, K, ws, out(0), lds, st);
     return hipGetLastError() == hipSuccess ? FLCE_OK : FLCE_ERR_HIP;
   }
   void* HT = p.fwd_copy ? ws + t.off_HT : nullptr;
@@ -90,12 +91,13 @@ flce_status run_topk(const TopkPlan& t, const void* H, const void* W, int K, cha
       a.nt0 = (int)(row0 / L::TILE); a.n_nt = (int)ceil_div(rows, L::TILE); a.n_vt = (int)ceil_div(V, L::TILE);
       a.stats = stats; a.ld_stats = t.ld_stats;
       a.z = z; a.ldz = t.ldz;
+      if (row0 == 0) a.zero = zero;
       {
         ProfScope ps(FLCE_PROF_FWD_TILES, st);
         launch_logit_tiles<T, L>(a, st);
       }
       ProfScope ps(FLCE_PROF_FWD_EPILOGUE, st);
-      launch_select(t, rows, row0, K, ws, logits, ids, lse, st);
+      launch_select(t, rows, K, ws, out(row0), lds, st);
     }
     return hipGetLastError() == hipSuccess ? FLCE_OK : FLCE_ERR_HIP;
   });
@@ -111,7 +113,7 @@ constexpr int REORDER_ROWS = 16;      // rows whose vectors a thread of the reor
 struct BeamPlan {
   TopkPlan t;
   int K;
-  int64_t off_logits, off_ids, off_lse, bytes;
+  int64_t off_cand, off_lse, off_arrived, bytes;
 };
 bool make_beam_plan(int64_t batch, int64_t beams, int64_t d, int64_t V, int64_t n_out, flce_dtype dt, BeamPlan& b) {
   if (batch < 1 || beams < 1 || beams > BEAMS_MAX || n_out < 1 || n_out > BEAMS_MAX || batch > 0x7FFFFF00ll / beams || V < 1) return false;
@@ -119,9 +121,9 @@ bool make_beam_plan(int64_t batch, int64_t beams, int64_t d, int64_t V, int64_t 
   if (!make_topk_plan(batch * beams, d, V, b.K, dt, b.t)) return false;
   const int64_t rows = batch * beams;
   int64_t o = b.t.bytes;
-  b.off_ids = o;    o = align_up(o + rows * b.K * 8, ALIGN);
-  b.off_logits = o; o = align_up(o + rows * b.K * 4, ALIGN);
-  b.off_lse = o;    o = align_up(o + rows * 4, ALIGN);
+  b.off_cand = o;    o = align_up(o + rows * b.K * 8, ALIGN);
+  b.off_lse = o;     o = align_up(o + rows * 4, ALIGN);
+  b.off_arrived = o; o = align_up(o + batch * 4, ALIGN);
   b.bytes = o;
   return true;
 }
@@ -149,7 +151,10 @@ flce_status flce_topk(const void* H, const void* W, int64_t N, int64_t d, int64_
   if (!flce::make_topk_plan(N, d, V, K, dt, t)) return FLCE_ERR_BAD_SHAPE;
   if (!flce::aligned16(H) || !flce::aligned16(W)) return FLCE_ERR_BAD_ARG;
   if (flce::bad_workspace(workspace, workspace_bytes, t.bytes)) return FLCE_ERR_WORKSPACE;
-  return flce::run_topk(t, H, W, (int)K, static_cast<char*>(workspace), logits_out, ids_out, lse_out, static_cast<hipStream_t>(hip_stream));
+  return flce::run_topk(
+      t, H, W, (int)K, static_cast<char*>(workspace),
+      [&](int64_t row0) { return flce::Largest{logits_out + row0 * K, ids_out + row0 * K, lse_out + row0}; }, 0, flce::ZeroWords{nullptr, 0},
+      static_cast<hipStream_t>(hip_stream));
 }
 
 size_t flce_beam_workspace_bytes(int64_t batch, int64_t beams, int64_t d, int64_t V, int64_t n_out, flce_dtype dt) {
@@ -173,15 +178,17 @@ flce_status flce_beam_step(const void* H, const void* W, const float* scores, co
   if (flce::bad_workspace(workspace, workspace_bytes, b.bytes)) return FLCE_ERR_WORKSPACE;
   char* ws = static_cast<char*>(workspace);
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  float* logits = reinterpret_cast<float*>(ws + b.off_logits);
-  int64_t* ids = reinterpret_cast<int64_t*>(ws + b.off_ids);
-  float* lse = reinterpret_cast<float*>(ws + b.off_lse);
-  const flce_status rc = flce::run_topk(b.t, H, W, b.K, ws, logits, ids, lse, st);
-  if (rc != FLCE_OK) return rc;
-  flce::ProfScope ps(FLCE_PROF_FWD_EPILOGUE, st);
-  flce::beam_select_kernel<<<(unsigned)batch, flce::SELECT_THREADS, (size_t)beams * (b.K + 1) * 4, st>>>(
-      logits, ids, lse, scores, finished, (int)beams, b.K, (int)n_out, eos_id, pad_id, scores_out, tokens_out, parents_out, finished_out);
-  return hipGetLastError() == hipSuccess ? FLCE_OK : FLCE_ERR_HIP;
+  uint32_t* arrived = reinterpret_cast<uint32_t*>(ws + b.off_arrived);
+  const flce::BeamStep out{scores, finished, 0, (int)beams, (int)n_out, eos_id, pad_id, scores_out, tokens_out, parents_out, finished_out,
+                           arrived, reinterpret_cast<unsigned long long*>(ws + b.off_cand), reinterpret_cast<float*>(ws + b.off_lse)};
+  return flce::run_topk(
+      b.t, H, W, b.K, ws,
+      [&](int64_t row0) {
+        flce::BeamStep o = out;
+        o.row0 = row0;
+        return o;
+      },
+      (size_t)beams * (b.K + 1) * 4, flce::ZeroWords{arrived, (int)batch}, st);
 }
 
 flce_status flce_beam_reorder(const void* src, void* dst, const int64_t* parents, int64_t outer, int64_t batch, int64_t beams_in,

@@ -92,6 +92,30 @@ def test_dead_and_odd_scores():
         assert len({(p, t) for p, t in zip(got[2][b], got[1][b])}) == 64 and (got[2][b] < 4).all() and (got[1][b] < 200).all()
 
 
+@pytest.mark.parametrize("dtype,batch,beams,d,V,n_out", [("bf16", 2, 3, 64, 900, 5), ("f32", 30, 4, 40, 700, 4), ("bf16", 60, 5, 8, 600_001, 3)])
+def test_outputs_and_workspace_end_where_they_say(dtype, batch, beams, d, V, n_out):
+    """Poisoned workspace, words behind every output; the last shape's rows go through in chunks that cut a search."""
+    rng = np.random.default_rng(8)
+    H, W = F.grid_operands(rng, batch * beams, d, V)
+    s = rng.standard_normal((batch, beams)).astype(np.float32)
+    code = {"bf16": B.FLCE_DTYPE_BF16, "f32": B.FLCE_DTYPE_F32}[dtype]
+    nb = B.flce_beam_workspace_bytes(batch, beams, d, V, n_out, code)
+    ws = torch.full((nb + 256,), 0xFF, dtype=torch.uint8, device="cuda")
+    n = batch * n_out
+    out = [torch.full((n + 32,), 9, dtype=t, device="cuda") for t in (torch.float32, torch.int64, torch.int64, torch.uint8)]
+    want = step(H.reshape(batch, beams, d), W, s, None, n_out, 3, 1, dtype)
+    for rep in range(2):                                  # the second time on what the first left in the workspace
+        assert B.flce_beam_step(F.on_gpu(H, dtype), F.on_gpu(W, dtype), torch.from_numpy(s).cuda(), None, batch, beams, d, V, n_out, 3, 1,
+                                code, *out, ws, nb) == B.FLCE_OK
+        torch.cuda.synchronize()
+        assert (ws[nb:] == 0xFF).all()
+        for x, w in zip(out, want):
+            assert (x[n:] == 9).all() and np.array_equal(x[:n].cpu().numpy().reshape(batch, n_out), w)
+    for b in (0, batch // 2, batch - 1):
+        one = F.beam(H.reshape(batch, beams, d)[b:b + 1], W, s[b:b + 1].astype(np.float64), None, n_out, 3, 1)
+        assert np.array_equal(want[1][b:b + 1], one[1]) and np.array_equal(want[2][b:b + 1], one[2])
+
+
 def test_a_graph_and_other_streams():
     rng = np.random.default_rng(7)
     batch, beams, d, V = 4, 4, 256, 8000
