@@ -17,14 +17,18 @@ __host__ __device__ __forceinline__ constexpr uint32_t list_entry(int row, int p
 }
 constexpr int LIST_BUCKETS = 8192;
 
-// Entries of each row tile sorted by vocabulary tile (in no order inside one: each has a place of its own to write to).
+// Entries of each row tile sorted by vocabulary tile and, inside it, by the wavefront that computes them (2 along the positions, NW along
+// the rows; in no order beyond that: each entry has a place of its own to write to).
 // One block per row tile: count, prefix sum, place.  A chain of latencies: a thread's first LIST_HELD entries are loaded together and
-// stay in registers (256 rows x 32 entries are all of them; 2048 rows 18.4 -> LISTS_US us), further ones are read twice.
+// stay in registers (256 rows x 32 entries are all of them), further ones are read twice, four at a time.  (2048 rows x 32 entries 18.4 us without that,
+// 11.0 with it.)
 constexpr int LIST_HELD = 8;
-template <int E>
+template <int E, int NW>
 __global__ __launch_bounds__(1024) void distill_lists_kernel(const int64_t* __restrict__ ids, const float* __restrict__ t, int N, int V, int K,
-                                                             int n_vt, int* __restrict__ list_begin, uint32_t* __restrict__ entries,
+                                                             int n_vt_all, int* __restrict__ list_begin, uint32_t* __restrict__ entries,
                                                              float2* __restrict__ saved, Header* __restrict__ hdr) {
+  constexpr int S = 2 * NW;
+  const int n_vt = n_vt_all * S;          // buckets
   __shared__ int cnt[LIST_BUCKETS];
   __shared__ int wsum[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -41,29 +45,39 @@ __global__ __launch_bounds__(1024) void distill_lists_kernel(const int64_t* __re
     float x[LIST_HELD];
 #pragma unroll
     for (int u = 0; u < LIST_HELD; ++u) {
+      if (u * 1024 >= total) break;
       const int i = min(tid + u * 1024, total - 1);
       id[u] = ids[i]; x[u] = t[i];
     }
 #pragma unroll
-    for (int u = 0; u < LIST_HELD; ++u) held[u] = tid + u * 1024 < total ? share_id(id[u], x[u]) : -1;
+    for (int u = 0; u < LIST_HELD; ++u)          // (all ones past the end, without a mask kept for each)
+      held[u] = u * 1024 < total ? share_id(id[u], x[u]) | ((total - 1 - tid - u * 1024) >> 31) : -1;
   }
   // f(i, id) for every entry with a share
   auto each = [&](auto f) {
 #pragma unroll
     for (int u = 0; u < LIST_HELD; ++u)
       if (held[u] >= 0) f(tid + u * 1024, held[u]);
-    for (int i = tid + LIST_HELD * 1024; i < total; i += 1024) {
-      const int id = share_id(ids[i], t[i]);
-      if (id >= 0) f(i, id);
+    for (int i0 = LIST_HELD * 1024; i0 < total; i0 += 4 * 1024) {
+      int id[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int i = min(i0 + u * 1024 + tid, total - 1);
+        id[u] = share_id(ids[i], t[i]);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (i0 + u * 1024 + tid < total && id[u] >= 0) f(i0 + u * 1024 + tid, id[u]);
     }
   };
+  auto bucket = [&](int i, int id) { return id / E * S + id % E / (E / 2) * NW + i / K / (E / NW); };
   int base = 0;
   for (int q0 = 0; q0 < n_vt; q0 += LIST_BUCKETS) {
     const int nq = min(LIST_BUCKETS, n_vt + 1 - q0);        // (with the one behind the last tile: the end)
     for (int i = tid; i < LIST_BUCKETS; i += 1024) cnt[i] = 0;
     __syncthreads();
-    each([&](int, int id) {
-      const int q = id / E - q0;
+    each([&](int i, int id) {
+      const int q = bucket(i, id) - q0;
       if (q >= 0 && q < LIST_BUCKETS) atomicAdd(&cnt[q], 1);
     });
     __syncthreads();
@@ -88,7 +102,7 @@ __global__ __launch_bounds__(1024) void distill_lists_kernel(const int64_t* __re
     for (int i = tid; i < nq; i += 1024) list_begin[q0 + i] = cnt[i];
     __syncthreads();
     each([&](int i, int id) {
-      const int q = id / E - q0;
+      const int q = bucket(i, id) - q0;
       if (q >= 0 && q < LIST_BUCKETS) entries[atomicAdd(&cnt[q], 1)] = list_entry(i / K, id % E, i % K);
     });
     base += all;
@@ -108,6 +122,13 @@ __device__ __forceinline__ void merge_scaled(const float (&m)[S], const float (&
   for (int k = 0; k < S; ++k) if (a[k] != 0.f) A += a[k] * fast_exp2((m[k] - M) * z_scale);
 }
 
+// Where the slices are: in the stage that the tuned loop leaves free between tiles, anywhere with the others.
+template <typename L>
+__host__ __device__ constexpr int list_lds() {
+  if constexpr (L::TUNED) return L::FREE_LDS_OFFSET;
+  else return 0;
+}
+
 template <typename T>
 struct DistillTileArgs {
   const T* H; const T* HT; const T* W;
@@ -116,20 +137,23 @@ struct DistillTileArgs {
   float z_scale;                        // log2(e) / T
   float* part; int64_t npad;            // [2][n_win][npad]: m, a per (window, row)
   int item_begin;
-  // per row tile TILE * K entries, those of vocabulary tile q from list_begin[q] to list_begin[q + 1]
+  // per row tile TILE * K entries, those of bucket b (vocabulary tile, wavefront) from list_begin[b] to list_begin[b + 1]
   const int* list_begin; const uint32_t* entries; int K; float2* saved;  // saved[row][place].y: the logit
 };
 
 // The forward's tiles: its walk over a window's vocabulary tiles, its online (m, a) in units of 1 / T, and after each tile the logits
-// that the lists name there, 64 entries at a time with one entry per lane: a block of accumulators that holds one (ballot) is
-// read once more and the owning lane stores it.  Bound by the matrix instructions; the tests for entries are one comparison per
-// block of 16 logits per lane.  The logit handed out is the one in the row's sum bit for bit, which exp(z - lse) - share needs where
-// both are near 1 (a dot product of its own would also read N K rows of W, 2.1 GB at 8192 x 4096 with 32 entries a row).
+// that the lists name there: a wavefront's entries 64 at a time, one per lane; a column of its blocks that holds some (ballot) goes through
+// the wavefront's slice of LDS, from where each entry's lane takes its logit, however many they are.  Bound by the matrix
+// instructions; a tile without entries costs a load and a comparison.  The logit handed out is the one in the row's sum bit
+// for bit, which exp(z - lse) - share needs where both are near 1 (a dot product of its own would also read N K rows of W, 2.1 GB
+// at 8192 x 4096 with 32 entries a row).
 template <typename T, typename L, bool HKR>
 __global__ __launch_bounds__(L::THREADS, L::MIN_WAVES) void distill_tiles_kernel(DistillTileArgs<T> a) {
   extern __shared__ __align__(16) char lds[];
   constexpr int COLS = L::ROWS == 64 ? 16 : 32;         // token columns of a block
-  const int lane = threadIdx.x & 63;
+  constexpr int POS = L::WM * L::ROWS;                  // positions of a wavefront's column of blocks
+  constexpr int NW = L::TILE / (L::WN * COLS);          // wavefronts along the rows
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int id = a.item_begin + xcd_contiguous_id(blockIdx.x, gridDim.x);
   int rb, win;
   grouped_raster(id, a.n_rb, a.n_win, FLCE_FWD_GROUP, rb, win);
@@ -141,7 +165,7 @@ __global__ __launch_bounds__(L::THREADS, L::MIN_WAVES) void distill_tiles_kernel
   // The lists run two tiles ahead: a tile's range is loaded while the tile before the last is computed, its first entries while the
   // last is, so that neither load is waited for ahead of a request.  A range is one vector register, its begin in even lanes
   // and its end in odd ones: the loop has no scalar registers for it.
-  auto load_range = [&](int vt) { return a.list_begin[(int64_t)rb * (a.n_vt + 1) + vt + (lane & 1)]; };
+  auto load_range = [&](int vt) { return a.list_begin[(int64_t)rb * (a.n_vt * 2 * NW + 1) + vt * 2 * NW + wave + (lane & 1)]; };
   auto load_entry = [&](int range, int first) {
     const int at = __builtin_amdgcn_readlane(range, 0) + first + lane;
     return at < __builtin_amdgcn_readlane(range, 1) ? a.entries[(int64_t)rb * (L::TILE * a.K) + at] : NO_ENTRY;
@@ -154,10 +178,12 @@ __global__ __launch_bounds__(L::THREADS, L::MIN_WAVES) void distill_tiles_kernel
   typename L::Acc acc;
   typename L::template Stream<HKR> stream;
   if (vt_begin < vt_end) {
-    range = load_range(vt_begin);
-    range_next = load_range(min(vt_begin + 1, a.n_vt - 1));
-    entry = load_entry(range, 0);
-    asm volatile("" : "+v"(entry), "+v"(range_next));
+    if constexpr (L::TUNED) {
+      range = load_range(vt_begin);
+      range_next = load_range(min(vt_begin + 1, a.n_vt - 1));
+      entry = load_entry(range, 0);
+      asm volatile("" : "+v"(entry), "+v"(range_next));
+    }
     stream.start(a.W, ld_bytes, vt_begin * L::TILE, a.V, a.H, a.HT, ld_bytes, n0, a.N, a.d, lds);
   }
   for (int vt = vt_begin; vt < vt_end; ++vt) {
@@ -166,8 +192,10 @@ __global__ __launch_bounds__(L::THREADS, L::MIN_WAVES) void distill_tiles_kernel
     int range2 = 0;
     stream.run(lds, acc, [&] {
       if (vt + 1 < vt_end) {
-        entry_next = load_entry(range_next, 0);
-        range2 = load_range(min(vt + 2, a.n_vt - 1));
+        if constexpr (L::TUNED) {
+          entry_next = load_entry(range_next, 0);
+          range2 = load_range(min(vt + 2, a.n_vt - 1));
+        }
         stream.start(a.W, ld_bytes, v0 + L::TILE, a.V, a.H, a.HT, ld_bytes, n0, a.N, a.d, lds);
       }
     });
@@ -200,40 +228,41 @@ __global__ __launch_bounds__(L::THREADS, L::MIN_WAVES) void distill_tiles_kernel
         __builtin_amdgcn_sched_barrier(0);     // one block at a time in VGPRs
       }
     }
+    if constexpr (!L::TUNED) {              // nothing is requested ahead, and no registers to spare across that main loop
+      range = load_range(vt);
+      entry = load_entry(range, 0);
+    }
     const int count = __builtin_amdgcn_readlane(range, 1) - __builtin_amdgcn_readlane(range, 0);
+    // [column][position], the 16-byte chunk number XOR-ed with the column: what a store or a read touches lies in different banks
+    float* slice = reinterpret_cast<float*>(lds + list_lds<L>() + wave * (COLS * POS * 4));
+    auto slot = [](int col, int chunk) { return col * POS + ((chunk ^ (col & (POS / 4 < 16 ? POS / 4 - 1 : 15))) << 2); };
     for (int c = 0; c < count; c += 64) {
       const uint32_t e = c == 0 ? entry : load_entry(range, c);
-      // the wavefront's block that holds the lane's entry, if one does (blocks are aligned to their size)
-      const int en = (int)(e & 255) - (L::tile_n(0) & ~(COLS - 1)), ev = (int)(e >> 8 & 255) - (L::tile_m(0, 0) & ~(L::ROWS - 1));
-      const bool mine = e != NO_ENTRY && en >= 0 && en < L::WN * COLS && ev >= 0 && ev < L::WM * L::ROWS;
-      const int block = mine ? en / COLS * L::WM + ev / L::ROWS : -1;
+      const int row = e & (L::WN * COLS - 1), pos = e >> 8 & (POS - 1);       // in the wavefront's part of the tile
+      const int ej = e != NO_ENTRY ? row / COLS : -1;
 #pragma unroll
       for (int j = 0; j < L::WN; ++j) {
+        if (__ballot(ej == j) == 0ull) continue;
+        int ln = lane;
+        asm volatile("" : "+v"(ln));          // (nothing derived from it is kept across the main loop)
+        const int col = ln & (COLS - 1);
 #pragma unroll
         for (int i = 0; i < L::WM; ++i) {
-          uint64_t hits = __ballot(block == j * L::WM + i);
-          if (hits != 0ull) {
-            float z[16];
 #pragma unroll
-            for (int r = 0; r < 16; ++r) z[r] = acc.get(i, j, r);
-            do {
-              const int from = __builtin_ctzll(hits);
-              hits &= hits - 1;
-              const uint32_t h = __builtin_amdgcn_readlane(e, from);
-              // row rel of a block is register 4 (rel / QUAD) + rel % 4 of the lanes of quarter (or half) rel % QUAD / 4
-              const int rel = h >> 8 & (L::ROWS - 1), in = rel % L::QUAD, r = rel / L::QUAD * 4 + (in & 3);
-              float v = z[0];
-#pragma unroll
-              for (int k = 1; k < 16; ++k) v = r == k ? z[k] : v;
-              if (lane == in / 4 * COLS + (int)(h & (COLS - 1))) a.saved[(int64_t)(n0 + (int)(h & 255)) * a.K + (h >> 16)].y = v;
-            } while (hits != 0ull);
-          }
+          for (int rq = 0; rq < 4; ++rq)
+            *reinterpret_cast<f32x4*>(slice + slot(col, (i * L::ROWS + rq * L::QUAD) / 4 + ln / COLS)) =
+                f32x4{acc.get(i, j, rq * 4), acc.get(i, j, rq * 4 + 1), acc.get(i, j, rq * 4 + 2), acc.get(i, j, rq * 4 + 3)};
           __builtin_amdgcn_sched_barrier(0);
         }
+        // (a wavefront's LDS operations complete in order)
+        if (ej == j) a.saved[(int64_t)(n0 + (int)(e & 255)) * a.K + (e >> 16)].y = slice[slot(row & (COLS - 1), pos / 4) + (pos & 3)];
       }
     }
-    asm volatile("" : "+v"(entry_next), "+v"(range2));
-    entry = entry_next; range = range_next; range_next = range2;
+    if constexpr (!L::TUNED) __syncthreads();       // the next tile's operands go where the slices are
+    if constexpr (L::TUNED) {
+      asm volatile("" : "+v"(entry_next), "+v"(range2));
+      entry = entry_next; range = range_next; range_next = range2;
+    }
   }
 
   // SLOTS lanes hold partial state of each token: merged in fixed slot order through LDS (free after the main loop's last barrier)
@@ -302,8 +331,11 @@ struct RowList {
 // The forward's end, a wavefront per row: lse from the windows' (m, a), the row's loss, and what the backward needs: shares (the
 // whole share of an id at its first place in the row, -1 at the others and where there is none) and the target that the row preparation
 // counts rows by (V: counts, matches no column; -1: does not count; V + 1: out of range).  Per-block sums in fixed order, and the
-// call's loss from them by the block that hands its sums in last (merge_rows_kernel's way).  A chain of latencies.
-constexpr int DISTILL_ROWS = 4;
+// call's loss from them by the block that hands its sums in last (merge_rows_kernel's way).  A chain of latencies; R rows per block:
+// 16, since the blocks count in one word, one after the other (7911 rows 15 us, in blocks of 4 31), but 4 where that leaves few blocks for a
+// list's comparisons (190 rows x 105 entries 10 us, in blocks of 16 16).
+constexpr int DISTILL_ROWS = 16, DISTILL_FEW_ROWS = 4, DISTILL_FEW = 1024;
+inline int distill_rows_per_block(int64_t N) { return N <= DISTILL_FEW ? DISTILL_FEW_ROWS : DISTILL_ROWS; }
 struct DistillRowArgs {
   const int64_t* ids; const float* t; float2* saved; int64_t* target;
   int N, V, K, n_win;
@@ -312,13 +344,13 @@ struct DistillRowArgs {
   float* lse_out; float* loss_rows_out;
   LossOut o;
 };
-static __global__ __launch_bounds__(64 * DISTILL_ROWS) void distill_rows_kernel(DistillRowArgs a) {
-  __shared__ int sid[DISTILL_ROWS][DISTILL_MAX];
-  __shared__ float sp[DISTILL_ROWS][DISTILL_MAX];
-  __shared__ float sl[DISTILL_ROWS];
-  __shared__ int sc[DISTILL_ROWS], so[DISTILL_ROWS], last;
+template <int R>
+__global__ __launch_bounds__(64 * R) void distill_rows_kernel(DistillRowArgs a) {
+  __shared__ int2 entry[R][DISTILL_MAX];        // (id, share's bits)
+  __shared__ float sl[R];
+  __shared__ int sc[R], so[R], last;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t n = (int64_t)blockIdx.x * DISTILL_ROWS + wave;
+  const int64_t n = (int64_t)blockIdx.x * R + wave;
   float loss = 0.f;
   bool counts = false, oor = false;
   if (n < a.N) {
@@ -332,10 +364,20 @@ static __global__ __launch_bounds__(64 * DISTILL_ROWS) void distill_rows_kernel(
     for (int u = 0; u < RowList::U; ++u) z[u] = lane + 64 * u < a.K ? saved[lane + 64 * u].y : 0.f;      // (undefined without a share)
     list.load(a.ids + n * a.K, a.t + n * a.K, a.K, a.V, a.inv_T);
 #pragma unroll
-    for (int u = 0; u < RowList::U; ++u) { sid[wave][lane + 64 * u] = list.id[u]; sp[wave][lane + 64 * u] = list.p[u]; }
-    for (int w = lane; w < a.n_win; w += 64) {
-      const float mw[2] = {m, pm[w * a.npad]}, aw[2] = {sum, pa[w * a.npad]};
-      merge_scaled<2>(mw, aw, a.z_scale, m, sum);
+    for (int u = 0; u < RowList::U; ++u) entry[wave][lane + 64 * u] = int2{list.id[u], __float_as_int(list.p[u])};
+    for (int w0 = 0; w0 < a.n_win; w0 += 4 * 64) {          // four windows per lane at a time, all their loads in flight together
+      float mw[5], aw[5];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int w = w0 + u * 64 + lane;
+        const int64_t at = (int64_t)min(w, a.n_win - 1) * a.npad;
+        mw[u] = pm[at]; aw[u] = pa[at];
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (w0 + u * 64 + lane >= a.n_win) { mw[u] = NEG_INF; aw[u] = 0.f; }
+      mw[4] = m; aw[4] = sum;
+      merge_scaled<5>(mw, aw, a.z_scale, m, sum);
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
@@ -351,18 +393,30 @@ static __global__ __launch_bounds__(64 * DISTILL_ROWS) void distill_rows_kernel(
       if (list.id[u] >= 0 && list.p[u] != 0.f) kl += list.p[u] * ((list.x[u] - list.log_sum) + fmaf(-z[u], a.inv_T, lse));
     kl = wave_sum(kl);
     loss = counts ? a.temperature * a.temperature * kl : 0.f;
+    // every entry against all of the row's, eight at a time (a wavefront reads what it wrote: LDS operations of one are in order)
+    float share[RowList::U];
+    int earlier[RowList::U];
+#pragma unroll
+    for (int u = 0; u < RowList::U; ++u) { share[u] = 0.f; earlier[u] = 0; }
+    for (int o0 = 0; o0 < a.K; o0 += 8) {          // (past K there are entries without an id)
+      int2 e[8];
+#pragma unroll
+      for (int o = 0; o < 8; ++o) e[o] = entry[wave][o0 + o];
+#pragma unroll
+      for (int u = 0; u < RowList::U; ++u) {
+        if (64 * u >= a.K) break;
+#pragma unroll
+        for (int o = 0; o < 8; ++o) {
+          const int same = e[o].x == list.id[u] ? -1 : 0;
+          share[u] += __int_as_float(e[o].y & same);
+          earlier[u] |= same & (o0 + o - (lane + 64 * u));        // (negative: an entry with the id stands before this one)
+        }
+      }
+    }
 #pragma unroll
     for (int u = 0; u < RowList::U; ++u) {
-      if (64 * u >= a.K) break;
       const int k = lane + 64 * u;
-      float share = 0.f;
-      bool first = list.id[u] >= 0;
-      for (int o = 0; o < a.K; ++o) {          // (a wavefront reads what it wrote: LDS operations of one are in order)
-        const bool same = sid[wave][o] == list.id[u];
-        if (same) share += sp[wave][o];
-        first = first && !(same && o < k);
-      }
-      if (k < a.K) saved[k] = float2{first ? share : -1.f, list.id[u] >= 0 ? z[u] : 0.f};
+      if (k < a.K) saved[k] = float2{list.id[u] >= 0 && earlier[u] >= 0 ? share[u] : -1.f, list.id[u] >= 0 ? z[u] : 0.f};
     }
     if (lane == 0) {
       a.lse_out[n] = lse;
@@ -376,7 +430,7 @@ static __global__ __launch_bounds__(64 * DISTILL_ROWS) void distill_rows_kernel(
     float l = 0.f;
     int c = 0, bad = 0;
 #pragma unroll
-    for (int w = 0; w < DISTILL_ROWS; ++w) { l += sl[w]; c += sc[w]; bad |= so[w]; }
+    for (int w = 0; w < R; ++w) { l += sl[w]; c += sc[w]; bad |= so[w]; }
     const int b = blockIdx.x;
     __hip_atomic_store(a.o.blk_loss + b, l, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __hip_atomic_store(a.o.blk_cnt + b, c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);

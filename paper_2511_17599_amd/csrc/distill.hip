@@ -54,9 +54,9 @@ bool make_distill_plan(int parts, int64_t N, int64_t d, int64_t V, int64_t K, fl
   const Plan& p = x.p;
   if (parts & PLAN_FORWARD) {
     x.tile = p.esize == 2 && !p.fast ? TILE : p.fwd_tile;
-    x.n_blk = (int)ceil_div(N, DISTILL_ROWS);
+    x.n_blk = (int)ceil_div(N, distill_rows_per_block(N));
     // The cross-entropy's windows, but in fp32 where they leave CUs idle as many as give every CU two workgroups, down to a tile each
-    // (its 64-row tiles are planned by 256 positions: 256 x 256 x 4096, 256 tiles of which 64 workgroups took four each, WIN_US us).
+    // (its 64-row tiles are planned by 256 positions: 256 x 256 x 4096, 256 tiles, 37 us as four each of 64 workgroups, 11 as one each).
     const int64_t rt = ceil_div(N, x.tile), vt = ceil_div(V, x.tile);
     x.n_win = p.n_win;
     if (p.esize == 4 && rt * x.n_win < 2 * NUM_CU) x.n_win = (int)std::min(vt, std::max<int64_t>(x.n_win, ceil_div(2 * NUM_CU, rt)));
@@ -66,7 +66,7 @@ bool make_distill_plan(int parts, int64_t N, int64_t d, int64_t V, int64_t K, fl
     x.off_blk_cnt = o;  o = align_up(o + (int64_t)x.n_blk * 4, ALIGN);
     x.off_blk_oor = o;  o = align_up(o + (int64_t)x.n_blk * 4, ALIGN);
     x.off_part = o;     o = align_up(o + 2ll * x.n_win * p.npad * 4, ALIGN);
-    x.off_begin = o;    o = align_up(o + n_rt * (n_vt + 1) * 4, ALIGN);
+    x.off_begin = o;    o = align_up(o + n_rt * (n_vt * (x.tile == TILE && !p.fast ? 8 : 4) + 1) * 4, ALIGN);
     x.off_entries = o;  o = align_up(o + n_rt * x.tile * K * 4, ALIGN);
     x.off_HT = o;       if (p.fwd_copy) o = align_up(o + packed_block_offset(p.n_rb, (int)d), ALIGN);
     x.fwd_bytes = o;
@@ -143,7 +143,7 @@ flce_status flce_distill_forward(const void* H, const void* W, const int64_t* te
     const int n_rb = (int)ceil_div(N, L::TILE), n_vt = (int)ceil_div(V, L::TILE), items = n_rb * x.n_win;
     {
       ProfScope ps(FLCE_PROF_FWD_EPILOGUE, st);
-      distill_lists_kernel<L::TILE><<<(unsigned)n_rb, 1024, 0, st>>>(teacher_ids, teacher_logits, (int)N, (int)V, (int)K, n_vt, begin, entries,
+      distill_lists_kernel<L::TILE, L::THREADS / 128><<<(unsigned)n_rb, 1024, 0, st>>>(teacher_ids, teacher_logits, (int)N, (int)V, (int)K, n_vt, begin, entries,
                                                                      saved, hdr);
     }
     {
@@ -165,11 +165,13 @@ flce_status flce_distill_forward(const void* H, const void* W, const int64_t* te
     ProfScope ps(FLCE_PROF_FWD_EPILOGUE, st);
     // a call for rows alone has no scalar loss to hand out: the sum goes to a spare word of the header block
     float* scalar = loss_out ? loss_out : reinterpret_cast<float*>(ws + 64);
-    distill_rows_kernel<<<x.n_blk, 64 * DISTILL_ROWS, 0, st>>>(DistillRowArgs{
+    const DistillRowArgs rows{
         teacher_ids, teacher_logits, saved, target, (int)N, (int)V, (int)K, x.n_win, part, p.npad, temperature, 1.f / temperature,
         LOG2E / temperature, lse_out, loss_rows_out,
         LossOut{reinterpret_cast<float*>(ws + x.off_blk_loss), reinterpret_cast<int*>(ws + x.off_blk_cnt),
-                reinterpret_cast<int*>(ws + x.off_blk_oor), hdr, scalar, reduction == FLCE_REDUCE_MEAN, nullptr, nullptr}});
+                reinterpret_cast<int*>(ws + x.off_blk_oor), hdr, scalar, reduction == FLCE_REDUCE_MEAN, nullptr, nullptr}};
+    if (N <= DISTILL_FEW) distill_rows_kernel<DISTILL_FEW_ROWS><<<x.n_blk, 64 * DISTILL_FEW_ROWS, 0, st>>>(rows);
+    else distill_rows_kernel<DISTILL_ROWS><<<x.n_blk, 64 * DISTILL_ROWS, 0, st>>>(rows);
     return hipGetLastError() == hipSuccess ? FLCE_OK : FLCE_ERR_HIP;
   });
 }

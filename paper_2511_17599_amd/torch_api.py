@@ -216,14 +216,19 @@ def linear_topk(H, W, k):
     return logits.reshape(*lead, k), ids.reshape(*lead, k), lse.reshape(lead)
 
 
+_eager_graphs = {}
+
+
 class _EagerGraph:
-    """Lives as long as the autograd graph of an eager distillation does."""
+    """Lives as long as the autograd graph of an eager distillation does; its leaves are known that long."""
+    __slots__ = ("key",)
 
     def __init__(self, leaves):
-        self.leaves = [weakref.ref(t) for t in leaves]
+        self.key = id(self)
+        _eager_graphs[self.key] = [weakref.ref(t) for t in leaves]
 
-
-_eager_graphs = weakref.WeakSet()
+    def __del__(self, graphs=_eager_graphs):
+        graphs.pop(self.key, None)
 
 
 def _graph_of(H, W):
@@ -234,12 +239,10 @@ def _graph_of(H, W):
     if not leaves or not torch.is_grad_enabled():
         return None
     if torch.cuda.is_available() and torch.cuda.is_current_stream_capturing():
-        if any(r() is t for g in _eager_graphs for r in g.leaves for t in leaves):
+        if any(r() is t for refs in list(_eager_graphs.values()) for r in refs for t in leaves):
             raise RuntimeError("an eager distillation of the same H or W is alive: drop its loss before capturing another")
         return None
-    graph = _EagerGraph(leaves)
-    _eager_graphs.add(graph)
-    return graph
+    return _EagerGraph(leaves)
 
 
 class _Distillation(torch.autograd.Function):
