@@ -319,8 +319,9 @@ flce_status flce_backward_partial(const void* H, const void* W_slice, const int6
  * The largest logits of each row, the N x V logits never kept: the K largest of row i of H.W^T in descending order, equal ones
  * (+0 and -0 among them) by ascending id, their ids, and the row's log-sum-exp over the whole vocabulary.  A NaN logit ranks
  * above every number (and makes the row's log-sum-exp NaN).  What a teacher's lists for flce_distill_forward are made of,
- * and what a sampler or a beam search chooses from.  Up to 32 rows (64 over a short
- * vocabulary) W is read once, straight to the matrix instructions; more rows go through the forward's main loop, a chunk of rows at a time whose logits wait in the workspace (fp32).
+ * and what a sampler or a beam search chooses from.  Up to 32 rows (64 over a short vocabulary) W is read once, straight to the
+ * matrix instructions; more rows go through the forward's main loop, a chunk of rows at a time whose logits wait in the
+ * workspace (fp32).
  *   K          : 1 .. 256, at most V.  V at most 2^22.
  *   logits_out : device, N*K floats.   ids_out : device, N*K int64.   lse_out : device, N floats.
  *   workspace  : flce_topk_workspace_bytes(N, d, V, K, dt) bytes (0: invalid shape): the logits of a chunk of rows (up to 1 GiB or 256

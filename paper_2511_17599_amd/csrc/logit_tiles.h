@@ -18,9 +18,11 @@ struct ZeroWords {
 template <typename T>
 struct LogitArgs {
   const T* H; const T* HT; const T* W;
-  int N, d, V, nt0, n_nt, n_vt;         // row tiles nt0 .. nt0 + n_nt - 1 by all vocabulary tiles
+  int N, d, V, nt0, n_nt, n_vt;         // row tiles nt0 .. nt0 + n_nt - 1 by vocabulary tiles vt0 .. vt0 + n_vt - 1
   float2* stats; int64_t ld_stats;      // [row - first row][group]: (max z, sum exp(z - max))
-  float* z; int64_t ldz;                // [row - first row][position], up to whole tiles
+  float* z; int64_t ldz;                // [row - first row][position], up to whole tiles; groups whose maximum is below the row's floor are not kept
+  const float* floor;                   // [row - first row], or null
+  int vt0;                              // first vocabulary tile
   ZeroWords zero;
 };
 
@@ -43,7 +45,7 @@ __device__ __forceinline__ float finite_or_zero(float m) { return fabsf(m) == __
 // one is post-processed).  A group is a block of L::ROWS consecutive positions, all of one wavefront: two or four lanes share a token.
 // Bound by the matrix instructions; per logit the post-processing adds an exponential and 4 bytes stored, 64 consecutive
 // ones of a row per store instruction.
-template <typename T, typename L, bool HKR>
+template <typename T, typename L, bool HKR, bool FLOOR>
 __global__ __launch_bounds__(L::THREADS, L::MIN_WAVES) void logit_tiles_kernel(LogitArgs<T> a) {
   extern __shared__ __align__(16) char lds[];
   constexpr int COLS = L::ROWS == 64 ? 16 : 32;         // token columns of a block
@@ -58,10 +60,22 @@ __global__ __launch_bounds__(L::THREADS, L::MIN_WAVES) void logit_tiles_kernel(L
   };
   typename L::template Stream<HKR> stream;
   auto start = [&](int p, int q) {
-    stream.start(a.W, ld_bytes, q * L::TILE, a.V, a.H, a.HT, ld_bytes, (a.nt0 + p) * L::TILE, a.N, a.d, lds);
+    stream.start(a.W, ld_bytes, (a.vt0 + q) * L::TILE, a.V, a.H, a.HT, ld_bytes, (a.nt0 + p) * L::TILE, a.N, a.d, lds);
+  };
+  // The rows' floors come with a tile's first requests (as the recompute step's inputs do), -inf without any.  A row past the end has
+  // +inf: nothing of it is kept.
+  float fl[L::WN], fl_next[L::WN];
+  const int rows = a.N - a.nt0 * L::TILE;
+  auto load_floor = [&](int p, float (&f)[L::WN]) {
+#pragma unroll
+    for (int j = 0; j < L::WN; ++j) {
+      const int n = p * L::TILE + L::tile_n(j);
+      f[j] = n >= rows ? __builtin_inff() : FLOOR ? a.floor[n] : NEG_INF;
+    }
   };
   int p, q;
   place(t, p, q);
+  if constexpr (L::TUNED) load_floor(p, fl);
   start(p, q);
   typename L::Acc acc;
   for (;;) {
@@ -69,13 +83,17 @@ __global__ __launch_bounds__(L::THREADS, L::MIN_WAVES) void logit_tiles_kernel(L
     const bool more = L::TUNED && t_next < total;      // (a loop with nothing to request ahead gets one tile per workgroup)
     int p_next = 0, q_next = 0;
     stream.run(lds, acc, [&] {
+      if constexpr (!L::TUNED) load_floor(p, fl);          // no registers to spare across that main loop
+#pragma unroll
+      for (int j = 0; j < L::WN; ++j) asm volatile("" : "+v"(fl[j]));
       if (more) {
         place(t_next, p_next, q_next);
+        load_floor(p_next, fl_next);
         start(p_next, q_next);
       }
     });
 
-    const int v0 = q * L::TILE, n0 = p * L::TILE;      // n0: relative to the launch's first row
+    const int v0 = (a.vt0 + q) * L::TILE, n0 = p * L::TILE;      // n0: relative to the launch's first row
     float2* __restrict__ stats = a.stats + (int64_t)n0 * a.ld_stats + v0 / L::ROWS;
 #pragma unroll
     for (int j = 0; j < L::WN; ++j) {
@@ -87,9 +105,6 @@ __global__ __launch_bounds__(L::THREADS, L::MIN_WAVES) void logit_tiles_kernel(L
         float z[16];
 #pragma unroll
         for (int r = 0; r < 16; ++r) z[r] = acc.get(i, j, r);
-#pragma unroll
-        for (int rq = 0; rq < 4; ++rq)
-          *reinterpret_cast<f32x4*>(zrow + blk + rq * L::QUAD) = f32x4{z[rq * 4], z[rq * 4 + 1], z[rq * 4 + 2], z[rq * 4 + 3]};
         if (v0 + blk + L::ROWS > a.V) {
           const int live = a.V - v0 - blk - L::lane_row();
 #pragma unroll
@@ -106,12 +121,27 @@ __global__ __launch_bounds__(L::THREADS, L::MIN_WAVES) void logit_tiles_kernel(L
         for (int r = 0; r < 16; ++r) sum += fast_exp2(fmaf(z[r], LOG2E, ms));
         sum = over_columns<COLS>(sum, [](float x, float y) { return x + y; });
         if (lane < COLS) stats[(int64_t)n * a.ld_stats + blk / L::ROWS] = float2{m, sum};
+        if (!(m < fl[j]) || (sum != sum && fl[j] < __builtin_inff())) {
+#pragma unroll
+          for (int rq = 0; rq < 4; ++rq)
+            *reinterpret_cast<f32x4*>(zrow + blk + rq * L::QUAD) = f32x4{z[rq * 4], z[rq * 4 + 1], z[rq * 4 + 2], z[rq * 4 + 3]};
+        }
         __builtin_amdgcn_sched_barrier(0);     // one block at a time in VGPRs
       }
     }
     if (!more) break;
     t = t_next; p = p_next; q = q_next;
+#pragma unroll
+    for (int j = 0; j < L::WN; ++j) { asm volatile("" : "+v"(fl_next[j])); fl[j] = fl_next[j]; }
   }
+}
+
+// Whether a loop's kernel has a form with floors: large calls alone need one, with the copy of H; the ragged hidden sizes' has no
+// scalar registers left for it.
+template <typename L>
+constexpr bool has_floors() {
+  if constexpr (L::TUNED) return std::is_same<L, typename L::Even>::value;
+  else return false;
 }
 
 template <typename T, typename L>
@@ -119,10 +149,11 @@ hipError_t logit_tiles_allowance() {
   static OncePerDevice once;
   return once([] {
     if constexpr (L::TUNED) {
-      const hipError_t e = allow_big_lds(logit_tiles_kernel<T, L, true>, L::LDS);
+      hipError_t e = allow_big_lds(logit_tiles_kernel<T, L, true, false>, L::LDS);
+      if constexpr (has_floors<L>()) { if (e == hipSuccess) e = allow_big_lds(logit_tiles_kernel<T, L, true, true>, L::LDS); }
       if (e != hipSuccess) return e;
     }
-    return allow_big_lds(logit_tiles_kernel<T, L, false>, L::LDS);
+    return allow_big_lds(logit_tiles_kernel<T, L, false, false>, L::LDS);
   });
 }
 
@@ -132,9 +163,12 @@ void launch_logit_tiles(const LogitArgs<T>& a, hipStream_t st) {
   int grid = a.n_nt * a.n_vt;
   if constexpr (L::TUNED) {
     if (grid > NUM_CU * L::PER_CU) grid = NUM_CU * L::PER_CU;
-    if (a.HT) { logit_tiles_kernel<T, L, true><<<grid, L::THREADS, L::LDS, st>>>(a); return; }
+    if constexpr (has_floors<L>()) {
+      if (a.HT && a.floor) { logit_tiles_kernel<T, L, true, true><<<grid, L::THREADS, L::LDS, st>>>(a); return; }
+    }
+    if (a.HT) { logit_tiles_kernel<T, L, true, false><<<grid, L::THREADS, L::LDS, st>>>(a); return; }
   }
-  logit_tiles_kernel<T, L, false><<<grid, L::THREADS, L::LDS, st>>>(a);
+  logit_tiles_kernel<T, L, false, false><<<grid, L::THREADS, L::LDS, st>>>(a);
 }
 
 }  // namespace flce

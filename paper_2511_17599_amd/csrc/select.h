@@ -199,7 +199,7 @@ __device__ __forceinline__ void arrive(const BeamStep& s, int K, int64_t row) {
 // Reads the groups' pairs once, where a thread's fit its registers, and some more than K groups of logits; a chain of latencies and seven
 // barriers.
 // OUT: Largest, or BeamStep with beams (K + 1) words of dynamic LDS.
-struct Largest { float* logits; int64_t* ids; float* lse; };      // [row][K], [row][K], [row] from the launch's first row on
+struct Largest { float* logits; int64_t* ids; float* lse; const float* floor; };    // [row][K], [row][K], [row], [row] or null; the launch's rows
 template <int G, typename OUT>      // positions per group
 __device__ __forceinline__ void select_row(const float* __restrict__ z, int64_t ldz, const float2* __restrict__ stats, int64_t ld_stats,
                                            int n_groups, int V, int K, const OUT& out) {
@@ -284,6 +284,8 @@ __device__ __forceinline__ void select_row(const float* __restrict__ z, int64_t 
   Bound b{0u, 0, n_groups};
   if (n_groups > want) b = find_bound(group_keys, lo, hi, want, want + max(16, want / 4), hist);
   int n_held = b.above + b.equal;
+  // below the row's floor, itself a lower bound of the K-th maximum, nothing was kept
+  if constexpr (!BEAM) { if (out.floor) b.low = max(b.low, order_key(out.floor[row])); }
   if (n_held <= SELECT_GROUPS) {
     append<int>([&](auto f) {
       if (held) {
@@ -295,6 +297,7 @@ __device__ __forceinline__ void select_row(const float* __restrict__ z, int64_t 
       }
     }, groups, SELECT_GROUPS, &word[0]);
     __syncthreads();
+    n_held = word[0];
   } else {
     n_held = want;
     collect_first([&](int g) { return group_key(stats[g]); }, n_groups, want, b, groups, word);
@@ -381,6 +384,34 @@ __global__ __launch_bounds__(SELECT_THREADS) void select_kernel(const float* __r
   } else {
     select_row<G>(z, ldz, stats, ld_stats, n_groups, V, K, out);
   }
+}
+
+// A lower bound of every row's K-th logit from its first n_groups groups (n_groups > K), one block per row: what the rest of the
+// vocabulary has to reach to be kept.  Finite or -inf: what lies above the largest number is kept whatever the floor.
+static __global__ __launch_bounds__(SELECT_THREADS) void floor_kernel(const float2* __restrict__ stats, int64_t ld_stats, int n_groups, int K,
+                                                                      float* __restrict__ floor) {
+  __shared__ __align__(16) int hist[4][256];
+  __shared__ uint32_t klo[SELECT_THREADS / 64], khi[SELECT_THREADS / 64];
+  const int t = threadIdx.x;
+  stats += (int64_t)blockIdx.x * ld_stats;
+  uint32_t lo = 0xFFFFFFFFu, hi = 0u;
+  for (int g = t; g < n_groups; g += SELECT_THREADS) {
+    const uint32_t k = group_key(stats[g]);
+    lo = min(lo, k); hi = max(hi, k);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    lo = min(lo, (uint32_t)__shfl_xor((int)lo, o, 64));
+    hi = max(hi, (uint32_t)__shfl_xor((int)hi, o, 64));
+  }
+#pragma unroll
+  for (int p = 0; p < 4; ++p) hist[p][t] = 0;
+  if ((t & 63) == 0) { klo[t >> 6] = lo; khi[t >> 6] = hi; }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < SELECT_THREADS / 64; ++w) { lo = min(lo, klo[w]); hi = max(hi, khi[w]); }
+  const Bound b = find_bound([&](auto f) { for (int g = t; g < n_groups; g += SELECT_THREADS) f(group_key(stats[g])); }, lo, hi, K, K + 2, hist);
+  if (t == 0) floor[blockIdx.x] = fminf(value_of(b.low), 3.402823466e38f);          // (NaN: the other operand)
 }
 
 // States of beams reordered: row (o, b, j) of dst = row (o, b, parents[b][j]) of src, row_bytes of it.

@@ -1,6 +1,7 @@
 // C-ABI entry points around a row's largest logits (see include/flce.h): the selection itself, a beam search's step on top of
 // it and the reordering of the beams' states.  Host code: checks, workspaces, launches.
 #include <algorithm>
+#include <cmath>
 
 #include "few_rows.h"
 #include "select.h"
@@ -17,15 +18,31 @@ struct TopkPlan {
   bool few;
   int group, n_groups;            // consecutive positions per group
   int64_t ldz, ld_stats, rows;    // rows of a chunk
-  int64_t off_z, off_stats, off_HT, bytes;
+  int first_vt;                   // vocabulary tiles of the first launch of a chunk where the others have a floor, 0: no such thing
+  int64_t off_z, off_stats, off_floor, off_HT, bytes;
 };
 
-bool make_topk_plan(int64_t N, int64_t d, int64_t V, int64_t K, flce_dtype dt, TopkPlan& t) {
+// A store of a tile's logits is drained before the next tile's K loop can wait for its operands (one counter for both): at 5 TB/s 13 us of a
+// 256-row tile that takes 95.  The K-th largest of the first positions' group maxima is a floor that most of the others' groups do not
+// reach, and those are not stored.  First part f of the vocabulary: the rest passes K / (f groups) of its groups, least in all at f = sqrt(K /
+// groups); whole rounds of workgroups, and only where both parts are several.  Without and with floors, us: 4096 x 4096 x 128256 K = 64 3348 /
+// 3112, K = 10 3294 / 3037; 4096 x 1024 x 50257 K = 20 510 / 437; 8192 x 768 x 50257 K = 100 1026 / 952; 8192 x 256 x 60000 K = 10 684 / 475.
+int first_tiles(int tile, const TopkPlan& t, int64_t K) {
+  const int64_t round = tile == TILE ? NUM_CU : 2 * NUM_CU;
+  const int64_t n_nt = ceil_div(std::min(t.rows, t.p.N), tile), n_vt = ceil_div(t.p.V, tile), per_round = std::max<int64_t>(1, round / n_nt);
+  const double f = std::max(1.0 / 16.0, std::sqrt((double)K / t.n_groups));
+  const int64_t first = align_up((int64_t)std::ceil(f * (double)n_vt), per_round);
+  const bool pays = f < 0.4 && n_nt * first >= 2 * round && n_nt * (n_vt - first) >= 4 * round && first * (tile / t.group) > 2 * K;
+  return pays ? (int)first : 0;
+}
+
+bool make_topk_plan(int64_t N, int64_t d, int64_t V, int64_t K, flce_dtype dt, TopkPlan& t, bool floors = true) {
   if (!make_plan(PLAN_FORWARD, N, d, V, dt, t.p)) return false;
   if (K < 1 || K > TOPK_MAX || K > V || V > TOPK_MAX_V) return false;
   const Plan& p = t.p;
   t.few = few_rows_ok(N, V);
   int64_t o = 0;
+  t.first_vt = 0;
   if (t.few) {
     t.group = few_rows_group(V);
     t.n_groups = (int)ceil_div(V, t.group);
@@ -40,9 +57,11 @@ bool make_topk_plan(int64_t N, int64_t d, int64_t V, int64_t K, flce_dtype dt, T
     t.ld_stats = vpad / t.group;
     const int64_t most = std::max<int64_t>(TILE, TOPK_STAGE_BYTES / (t.ldz * 4) / TILE * TILE);
     t.rows = align_up(ceil_div(p.npad, ceil_div(p.npad, most)), TILE);
+    if (floors && p.fwd_copy && !p.ragged) t.first_vt = first_tiles(p.fwd_tile, t, K);
   }
   t.off_z = o;     o = align_up(o + t.rows * t.ldz * 4, ALIGN);
   t.off_stats = o; o = align_up(o + t.rows * t.ld_stats * 8, ALIGN);
+  t.off_floor = o; o = align_up(o + t.rows * 4, ALIGN);
   t.off_HT = o;    if (!t.few && p.fwd_copy) o = align_up(o + packed_block_offset(p.n_rb, (int)d), ALIGN);
   t.bytes = o;
   return true;
@@ -92,6 +111,22 @@ flce_status run_topk(const TopkPlan& t, const void* H, const void* W, int K, cha
       a.stats = stats; a.ld_stats = t.ld_stats;
       a.z = z; a.ldz = t.ldz;
       if (row0 == 0) a.zero = zero;
+      if (t.first_vt) {
+        float* floor = reinterpret_cast<float*>(ws + t.off_floor);
+        const int all = a.n_vt;
+        a.n_vt = t.first_vt;
+        {
+          ProfScope ps(FLCE_PROF_FWD_TILES, st);
+          launch_logit_tiles<T, L>(a, st);
+        }
+        {
+          ProfScope ps(FLCE_PROF_FWD_EPILOGUE, st);
+          floor_kernel<<<(unsigned)rows, SELECT_THREADS, 0, st>>>(stats, t.ld_stats, t.first_vt * (L::TILE / t.group), K, floor);
+        }
+        a.vt0 = t.first_vt; a.n_vt = all - t.first_vt;
+        a.floor = floor;
+        a.zero.n = 0;
+      }
       {
         ProfScope ps(FLCE_PROF_FWD_TILES, st);
         launch_logit_tiles<T, L>(a, st);
@@ -118,7 +153,7 @@ struct BeamPlan {
 bool make_beam_plan(int64_t batch, int64_t beams, int64_t d, int64_t V, int64_t n_out, flce_dtype dt, BeamPlan& b) {
   if (batch < 1 || beams < 1 || beams > BEAMS_MAX || n_out < 1 || n_out > BEAMS_MAX || batch > 0x7FFFFF00ll / beams || V < 1) return false;
   b.K = (int)std::min(n_out, V);
-  if (!make_topk_plan(batch * beams, d, V, b.K, dt, b.t)) return false;
+  if (!make_topk_plan(batch * beams, d, V, b.K, dt, b.t, /*floors=*/false)) return false;
   const int64_t rows = batch * beams;
   int64_t o = b.t.bytes;
   b.off_cand = o;    o = align_up(o + rows * b.K * 8, ALIGN);
@@ -151,9 +186,10 @@ flce_status flce_topk(const void* H, const void* W, int64_t N, int64_t d, int64_
   if (!flce::make_topk_plan(N, d, V, K, dt, t)) return FLCE_ERR_BAD_SHAPE;
   if (!flce::aligned16(H) || !flce::aligned16(W)) return FLCE_ERR_BAD_ARG;
   if (flce::bad_workspace(workspace, workspace_bytes, t.bytes)) return FLCE_ERR_WORKSPACE;
+  const float* floor = t.first_vt ? reinterpret_cast<const float*>(static_cast<char*>(workspace) + t.off_floor) : nullptr;
   return flce::run_topk(
       t, H, W, (int)K, static_cast<char*>(workspace),
-      [&](int64_t row0) { return flce::Largest{logits_out + row0 * K, ids_out + row0 * K, lse_out + row0}; }, 0, flce::ZeroWords{nullptr, 0},
+      [&](int64_t row0) { return flce::Largest{logits_out + row0 * K, ids_out + row0 * K, lse_out + row0, floor}; }, 0, flce::ZeroWords{nullptr, 0},
       static_cast<hipStream_t>(hip_stream));
 }
 

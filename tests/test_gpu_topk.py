@@ -77,6 +77,42 @@ def test_the_copy_of_h():
         assert torch.equal(z[:, 0], full.max(1).values)
 
 
+@pytest.mark.parametrize("knobs,N,d,V,K", [(dict(), 2100, 1024, 50000, 5), (dict(), 2100, 1024, 50000, 60), (dict(FLCE_TILE=128), 1100, 1024, 60000, 20)])
+def test_floors(monkeypatch, knobs, N, d, V, K):
+    """Calls of many rounds keep only the groups that reach a floor from the vocabulary's first part: rows whose largest logits all lie
+    in that part, all behind it, are all equal, NaN, infinite or -inf."""
+    set_plan(monkeypatch, **knobs)
+    rng = np.random.default_rng(V + K)
+    H, W = F.grid_operands(rng, N, d, V)
+    H[0] = 0
+    W[:, :4] = 0
+    H[:, :4] = 0
+    H[1:40, 0], W[:200, 0] = 7, 0.12                      # large at the start
+    H[1:20, 1], W[V - 300:, 1] = 7, 0.12                  # and at the end
+    H[40:60, 2], W[V // 2:, 2] = -7.9375, 0.12            # low behind the middle
+    Hg, Wg = F.on_gpu(H, "bf16"), F.on_gpu(W, "bf16")
+
+    def compare(rows):
+        z, ids, lse = call(Hg, Wg, K)
+        full = Hg[rows].float() @ Wg.float().t()
+        wz, wids, wlse = F.topk(F.f64(full), K)
+        assert np.array_equal(ids[rows].cpu().numpy(), wids) and np.array_equal(F.f64(z[rows]), wz, equal_nan=True)
+        fin = np.isfinite(wlse)
+        got = F.f64(lse[rows])
+        assert (np.abs(got[fin] - wlse[fin]) <= F.lse_bound(wlse[fin], V)).all() and np.array_equal(got[~fin], wlse[~fin], equal_nan=True)
+
+    compare(slice(0, 64))
+    compare(slice(N - 64, N))
+    Wg[7, 3] = float("inf")                               # K and more infinities in the first part for rows 2 .. 9, NaN behind it
+    Wg[100:100 + 64 * K:64, 3] = float("inf")
+    Wg[V - 9, 3] = float("nan")
+    Hg[2:10, 3] = 1
+    Hg[10:12, 3] = -1
+    torch.cuda.synchronize()
+    z, ids, lse = call(Hg[:N].contiguous(), Wg, K)
+    assert (ids[2:12, 0] == V - 9).all() and torch.isnan(z[:, 0]).all()      # (0 times an infinity: every row)
+
+
 @pytest.mark.parametrize("N", [3, 70])
 def test_more_groups_than_lds_holds_and_chunks_of_rows(N):
     V, d = 600_001, 8
