@@ -29,8 +29,9 @@ def test_topk_workspace():
     for bad in ((0, 64, 512, 4), (8, 63, 512, 4), (8, 64, 512, 0), (8, 64, 512, 513), (8, 64, 3, 4)):
         assert B.flce_topk_workspace_bytes(*bad, BF16) == 0
     assert B.flce_topk_workspace_bytes(8, 64, 512, 4, 5) == 0
-    # a few rows: their logits; many: a chunk's, however many
-    assert B.flce_topk_workspace_bytes(64, 4096, 128256, 64, BF16) < 64 * 128256 * 4 * 1.1
+    # a few rows: their logits; more: whole tiles of 256 rows, a chunk of them however many
+    assert B.flce_topk_workspace_bytes(32, 4096, 128256, 64, BF16) < 32 * 128256 * 4 * 1.1
+    assert B.flce_topk_workspace_bytes(64, 4096, 128256, 64, BF16) < 256 * 128256 * 4 * 1.1
     for N in (8192, 131072):
         assert B.flce_topk_workspace_bytes(N, 4096, 128256, 64, BF16) < (1 << 30) * 1.05 + N * 4096 * 2 * 1.01 + (1 << 20)
 
