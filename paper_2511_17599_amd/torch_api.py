@@ -143,6 +143,33 @@ class _RowLosses(torch.autograd.Function):
         return dH if dH.shape == shape else dH.reshape(shape), dW, None, None, None
 
 
+_eager_graphs = {}
+
+
+class _EagerGraph:
+    """Lives as long as the autograd graph of an eager loss does; its leaves are known that long."""
+    __slots__ = ("key",)
+
+    def __init__(self, leaves):
+        self.key = id(self)
+        _eager_graphs[self.key] = [weakref.ref(t) for t in leaves]
+
+    def __del__(self, graphs=_eager_graphs):
+        graphs.pop(self.key, None)
+
+
+def _leaves(H, W):
+    return [t for t in (H, W) if t.requires_grad and t.is_leaf] if torch.is_grad_enabled() else []
+
+
+def _known(loss, H, W):
+    """`loss` with its leaves known as long as its graph lives (see _graph_of)."""
+    leaves = _leaves(H, W)
+    if leaves and loss.is_cuda and not torch.cuda.is_current_stream_capturing():
+        loss.grad_fn.graph = _EagerGraph(leaves)
+    return loss
+
+
 def linear_cross_entropy(H, W, targets, ignore_index=-100, reduction="mean", label_smoothing=0.0):
     """Cross-entropy of softmax(H . W^T) against `targets` without the logits tensor.
 
@@ -155,8 +182,8 @@ def linear_cross_entropy(H, W, targets, ignore_index=-100, reduction="mean", lab
     if reduction != "none":
         if label_smoothing != 0.0:
             raise ValueError("label smoothing is available with reduction='none' only")
-        return _ScalarLoss.apply(H, W, targets, int(ignore_index), reduction)
-    return _RowLosses.apply(H, W, targets, int(ignore_index), float(label_smoothing))
+        return _known(_ScalarLoss.apply(H, W, targets, int(ignore_index), reduction), H, W)
+    return _known(_RowLosses.apply(H, W, targets, int(ignore_index), float(label_smoothing)), H, W)
 
 
 def _launch(call, device, *args):
@@ -216,31 +243,16 @@ def linear_topk(H, W, k):
     return logits.reshape(*lead, k), ids.reshape(*lead, k), lse.reshape(lead)
 
 
-_eager_graphs = {}
-
-
-class _EagerGraph:
-    """Lives as long as the autograd graph of an eager distillation does; its leaves are known that long."""
-    __slots__ = ("key",)
-
-    def __init__(self, leaves):
-        self.key = id(self)
-        _eager_graphs[self.key] = [weakref.ref(t) for t in leaves]
-
-    def __del__(self, graphs=_eager_graphs):
-        graphs.pop(self.key, None)
-
-
 def _graph_of(H, W):
     """While an autograd graph made outside a HIP graph's capture lives, torch's gradient accumulators of its leaves belong to the
     stream it was made on; a backward captured for the same leaves would wait for that stream, which ends the process.  Such a
     capture is refused."""
-    leaves = [t for t in (H, W) if t.requires_grad and t.is_leaf]
-    if not leaves or not torch.is_grad_enabled():
+    leaves = _leaves(H, W)
+    if not leaves:
         return None
-    if torch.cuda.is_available() and torch.cuda.is_current_stream_capturing():
+    if H.is_cuda and torch.cuda.is_current_stream_capturing():
         if any(r() is t for refs in list(_eager_graphs.values()) for r in refs for t in leaves):
-            raise RuntimeError("an eager distillation of the same H or W is alive: drop its loss before capturing another")
+            raise RuntimeError("an eager loss of the same H or W is alive: drop it before capturing a distillation")
         return None
     return _EagerGraph(leaves)
 
@@ -362,7 +374,7 @@ def reorder_states(parents, states, out=None, dim=1, status=None):
     parents [batch, beams_out] (int64); dimension `dim` of `states` is the batch, the next one the beams; what lies ahead of it
     (layers, keys and values) may be strided once, a beam's row is contiguous.  out: a tensor of states' shape with beams_out
     beams (a new one by default); out=states reorders in place (up to 16 beams).  status: an int32 tensor that becomes
-    FLCE_ERR_TARGET_RANGE where a parent is no beam (whose row is left as it was).  Returns out.
+    FLCE_ERR_TARGET_RANGE where a parent is no beam (whose row is left as it was).  Returns out.  Not differentiable.
     """
     if not states.is_cuda or parents.device != states.device or (out is not None and out.device != states.device):
         raise ValueError("parents, states and out must be on one GPU")

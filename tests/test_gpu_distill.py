@@ -334,6 +334,20 @@ def test_capture_beside_a_living_eager_graph_is_refused(monkeypatch):
     assert linear_distillation(H, W, ids, t).item() == value
 
 
+@pytest.mark.parametrize("reduction", ["mean", "none"])
+def test_capture_beside_a_living_eager_cross_entropy_is_refused(monkeypatch, reduction):
+    """(The check alone, as above.)  The refusal ends with the graph of the loss, not with the loss's own name."""
+    H, W = torch.randn(8, 16, device="cuda", requires_grad=True), torch.randn(30, 16, device="cuda", requires_grad=True)
+    ids, t = torch.zeros(8, 2, dtype=torch.int64, device="cuda"), torch.zeros(8, 2, device="cuda")
+    y = torch.zeros(8, dtype=torch.int64, device="cuda")
+    loss = 2 * linear_cross_entropy(H, W, y, reduction=reduction)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    with pytest.raises(RuntimeError, match="alive"):
+        linear_distillation(H, W, ids, t)
+    del loss
+    linear_distillation(H, W, ids, t)
+
+
 def test_teacher_to_student():
     """A teacher's lists as linear_topk writes them, and a student trained on them: the losses are the definition's on those lists."""
     rng = np.random.default_rng(23)
