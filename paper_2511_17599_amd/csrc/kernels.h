@@ -14,7 +14,7 @@
 //             pack_rows_kernel (the forward's pre-tiled copy of H for the tuned loop, where
 //             it pays); transpose_pad_kernel (generic loop: the K-contiguous copy of W that the
 //             dH contraction needs)
-//             recompute_kernel (Alg. 2: z recomputed, g = p - onehot, staged once in a
+//             recompute_kernel (recompute.h; Alg. 2: z recomputed, g = p - onehot, staged once in a
 //             fixed-size buffer; the generic loop also stages the transpose)
 //             contract_kernel (Eq. 4 and Eq. 5 as output-stationary MFMA
 //             contractions with a fixed chunk order; Gamma applied at the flush);
