@@ -166,6 +166,26 @@ def test_reorder(dtype, outer, batch, bi, bo, n):
         assert reorder_states(par, same, out=same) is same and torch.equal(same, plain_reorder(src, par))
 
 
+@pytest.mark.parametrize("pad", [0, 12])
+def test_reorder_states_beyond_32_bits(pad):
+    """Rows of more than 2^31 bytes, slabs of more than 2^32, as wide vectors and (pad: rows 4 bytes off) as narrow ones; in place too."""
+    n = (1 << 31) + 64
+    src = torch.empty(2, 1, 2, n + pad, dtype=torch.uint8, device="cuda")
+    for o in range(2):
+        for j in range(2):
+            src[o, 0, j] = (torch.arange(n + pad, device="cuda") % 251 + 2 * o + j).to(torch.uint8)
+    par = torch.tensor([[1, 0]], device="cuda")
+    part = src[..., :n]
+    moved = reorder_states(par, part)
+    for o in range(2):
+        for j in range(2):
+            assert torch.equal(moved[o, 0, j], part[o, 0, 1 - j])
+    reorder_states(par, part, out=part)
+    for o in range(2):
+        for j in range(2):
+            assert torch.equal(moved[o, 0, j], part[o, 0, j])
+
+
 def test_reorder_rows_of_odd_addresses_and_in_place_parts():
     par = torch.tensor([[1, 1, 0], [2, 0, 1]], device="cuda")
     base = torch.arange(4 * 6 * 37 + 5, device="cuda").to(torch.uint8)

@@ -119,6 +119,12 @@ def test_every_loop_and_chunks(monkeypatch, knobs, d, per_row):
     check(np.random.default_rng(7), 700, d, 3333, 40, "bf16", 1.5, "mean", "wild", per_row)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [0.05, 40.0])
+def test_far_temperatures(dtype, T):
+    check(np.random.default_rng(13), 210, 72, 1500, 30, dtype, T, "mean", "wild", False)
+
+
 @pytest.mark.parametrize("edges,N,d,V", [((64, 64), 300, 96, 3000), ((128, 128), 1300, 96, 4100)])
 def test_f32_edges_in_chunks(monkeypatch, edges, N, d, V):
     set_plan(monkeypatch, FLCE_VC_TILES=5, FLCE_NC_TILES=2)

@@ -134,6 +134,21 @@ def test_rows_in_several_chunks():
         assert (np.abs(F.f64(lse[i:i + 1]) - wlse) <= F.lse_bound(wlse, V)).all()
 
 
+@pytest.mark.parametrize("N", [2, 40, 300])
+def test_w_beyond_32_bits_of_bytes(N):
+    """Largest logits whose rows of W lie on both sides of 2^31 and 2^32 bytes."""
+    V, d = 600_007, 4096                                  # 4.9 GB
+    W = torch.zeros(V, d, dtype=torch.bfloat16, device="cuda")
+    at = [V - 1, (1 << 32) // (2 * d), (1 << 32) // (2 * d) - 1, (1 << 31) // (2 * d), 0, V - 300]
+    for i, v in enumerate(at):
+        W[v, d - 1 - i] = 6 - i
+    H = torch.ones(N, d, dtype=torch.bfloat16, device="cuda")
+    z, ids, lse = call(H, W, 8)
+    assert ids.tolist() == [at + [1, 2]] * N and z.tolist() == [[6., 5., 4., 3., 2., 1., 0., 0.]] * N
+    want = np.log(V - 6 + np.exp(np.arange(1.0, 7.0)).sum())
+    assert (np.abs(F.f64(lse) - want) <= F.lse_bound(want, V)).all()
+
+
 @pytest.mark.parametrize("N", [4, 130])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("K", [1, 60, 256])
