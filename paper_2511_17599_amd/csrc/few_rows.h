@@ -124,10 +124,10 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void few_rows_kernel(const T* __res
     }
 #pragma unroll
     for (int o = 1; o < TPT; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-    const float ms = -finite_or_zero(m) * LOG2E;
+    const float ref = finite_or_zero(m);
     float sum = 0.f;
 #pragma unroll
-    for (int e = 0; e < VPT; ++e) sum += fast_exp2(fmaf(x[e], LOG2E, ms));
+    for (int e = 0; e < VPT; ++e) sum += fast_exp2((x[e] - ref) * LOG2E);
 #pragma unroll
     for (int o = 1; o < TPT; o <<= 1) sum += __shfl_xor(sum, o, 64);
     if (n < N) {

@@ -38,7 +38,8 @@ __device__ __forceinline__ float over_columns(float v, F f) {
   return f(__uint_as_float(x[0]), __uint_as_float(x[1]));
 }
 // The value a group's exponentials are taken relative to: its maximum, but 0 where there is none (all -inf) and where it is
-// +inf: the sum is then 0 or +inf, and NaN only where a logit is NaN.
+// +inf: the sum is then 0 or +inf, and NaN only where a logit is NaN.  Subtracted before the factor log2(e): the product of a logit
+// beyond 2.36e38 with it (a vocabulary masked with the type's lowest value) is no number, the difference has none such.
 __device__ __forceinline__ float finite_or_zero(float m) { return fabsf(m) == __builtin_inff() ? 0.f : m; }
 
 // Workgroups walk the tiles as the recompute step's do (same raster, the next tile's first K stages requested before the current
@@ -115,10 +116,10 @@ __global__ __launch_bounds__(L::THREADS, L::MIN_WAVES) void logit_tiles_kernel(L
 #pragma unroll
         for (int r = 1; r < 16; ++r) m = fmaxf(m, z[r]);
         m = over_columns<COLS>(m, [](float x, float y) { return fmaxf(x, y); });
-        const float ms = -finite_or_zero(m) * LOG2E;
+        const float ref = finite_or_zero(m);
         float sum = 0.f;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sum += fast_exp2(fmaf(z[r], LOG2E, ms));
+        for (int r = 0; r < 16; ++r) sum += fast_exp2((z[r] - ref) * LOG2E);
         sum = over_columns<COLS>(sum, [](float x, float y) { return x + y; });
         if (lane < COLS) stats[(int64_t)n * a.ld_stats + blk / L::ROWS] = float2{m, sum};
         if (!(m < fl[j]) || (sum != sum && fl[j] < __builtin_inff())) {

@@ -1,0 +1,68 @@
+"""GPU: logits near the largest number of 32 bits (vocabularies masked with the type's lowest value, whole groups of them, whole rows,
+the end of the vocabulary) through every call that keeps a few logits per row.  The masks come in as a column of W that some rows of H
+multiply by one: such a logit is the mask's value exactly, whatever the other columns add to it."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+import few_logits as F                                    # noqa: E402
+import test_gpu_topk as TK                                # noqa: E402
+from conftest import set_plan                             # noqa: E402
+
+LOW = float(torch.finfo(torch.bfloat16).min)              # -3.39e38, held by both types
+HIGH = -LOW
+
+
+def masked_operands(rng, N, d, V):
+    """Column 0: groups are masked (in all rows but 1, 3 and the last of five or more); row 1: every logit is; row 2: one large logit; row 3:
+    all but three are masked."""
+    H, W = F.grid_operands(rng, N, d, V)
+    H[:, :4], W[:, :4] = 0, 0
+    H[:, 0] = 1
+    W[:min(64, V // 2), 0] = LOW
+    W[V // 2:V // 2 + V // 4, 0] = LOW                    # groups in the middle, each whole
+    W[V - V // 16 - 1:, 0] = LOW                          # and the last ones, whatever the last one holds
+    if N > 3:
+        H[1, :2] = 0, 1
+        W[:, 1] = LOW
+        H[2, 2] = 1
+        W[V // 2 - 1, 2] = HIGH
+        H[3, 0], H[3, 3] = 0, 1
+        W[:, 3] = LOW
+        W[V // 2 - 3:V // 2, 3] = 0
+    if N > 4:
+        H[N - 1, 0] = 0
+    return H, W
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("K", [1, 20, 200])
+@pytest.mark.parametrize("N,d,V", [(1, 8, 300), (4, 64, 301), (5, 72, 20011), (4, 64, 40007), (20, 64, 66003), (64, 64, 333), (70, 96, 333), (300, 104, 5003)])
+def test_masks_in_topk(dtype, K, N, d, V):
+    H, W = masked_operands(np.random.default_rng(V + N), N, d, V)
+    TK.check(H, W, K, dtype)
+
+
+@pytest.mark.parametrize("knobs", [dict(FLCE_GENERIC=1), dict(FLCE_TILE=128), dict(FLCE_TILE=256)])
+def test_masks_in_every_loop(monkeypatch, knobs):
+    set_plan(monkeypatch, **knobs)
+    H, W = masked_operands(np.random.default_rng(4), 300, 96, 3333)
+    TK.check(H, W, 20, "bf16")
+
+
+@pytest.mark.parametrize("K", [1, 60])
+def test_masks_beside_a_floor(K):
+    """Many rounds of tiles: what the vocabulary's first part gives as a floor for the rest."""
+    N, d, V = 2100, 1024, 50000
+    rng = np.random.default_rng(K)
+    H, W = masked_operands(rng, N, d, V)
+    Hg, Wg = F.on_gpu(H, "bf16"), F.on_gpu(W, "bf16")
+    z, ids, lse = TK.call(Hg, Wg, K)
+    for rows in (slice(0, 40), slice(N - 40, N)):
+        full = Hg[rows].float() @ Wg.float().t()
+        wz, wids, wlse = F.topk(F.f64(full), K)
+        assert np.array_equal(ids[rows].cpu().numpy(), wids) and np.array_equal(F.f64(z[rows]), wz)
+        assert (np.abs(F.f64(lse[rows]) - wlse) <= F.lse_bound(wlse, V)).all()
