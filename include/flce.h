@@ -370,7 +370,7 @@ flce_status flce_distill_backward(const void* H, const void* W, const int64_t* t
 /*
  * One step of a beam search.  `batch` searches of `beams` beams; beam j of search b has the hidden state H[b * beams + j], the score
  * scores[b][j] (a sum of log-probabilities) and, if `finished` is not NULL, a flag.  Candidates of a search: for a beam that
- * goes on every token v with scores[b][j] + (Z_v - lse), for a finished one (flag not 0) itself, with its score and pad_id.  The
+ * goes on every token v with scores[b][j] + log softmax(Z)_v, for a finished one (flag not 0) itself, with its score and pad_id.  The
  * n_out best in descending order, equal scores by beam, then by logit, then by token; a beam whose score is NaN or +inf
  * hands it to all its candidates, and NaN ranks above every number.  n_out may differ from beams (a first step widens one beam
  * to several; twice the beams leave a choice to the caller).  Where there are fewer candidates than n_out, the rest have

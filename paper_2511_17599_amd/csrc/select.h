@@ -115,11 +115,12 @@ struct BeamStep {
   float* scores_out; int64_t* tokens_out; int64_t* parents_out; uint8_t* finished_out;
   uint32_t* arrived;                // [search], zero
   unsigned long long* cand;         // [row][K]: (key, ~id) in order
-  float* lse;                       // [row]
+  unsigned long long* norm;         // [row]: (M, log sum exp(z - M)), M the largest logit
   __device__ __forceinline__ bool done(int64_t row) const { return finished && finished[row]; }
 };
 
-// Scores of a beam's candidates are in order as its logits are; a finished beam is its own one candidate.  A candidate's rank is its
+// Scores of a beam's candidates, s + ((z - M) - log sum exp(z - M)), are in order as its logits are: z - (M + log sum) would lose the
+// logarithm beside a large M (a beam whose logits are all the mask's value is uniform, -log V).  A finished beam is its own one candidate.  A candidate's rank is its
 // place in its own beam's list plus the number of candidates of the other beams that come before it (a binary search in each list):
 // larger score first, equal ones by beam.  key: [beams][K], len: [beams] in LDS.
 __device__ __forceinline__ void rank_beams(const BeamStep& s, int K, int64_t search, uint32_t* key, int* len) {
@@ -131,8 +132,10 @@ __device__ __forceinline__ void rank_beams(const BeamStep& s, int K, int64_t sea
     const int j = i / K;
     float x = s.scores[row0 + j];
     // (NaN and +inf stay what they are, so that a beam's scores are in order whatever its logits)
-    if (!s.done(row0 + j) && x < __builtin_inff())
-      x += value_of((uint32_t)(pair(i) >> 32)) - __hip_atomic_load(s.lse + row0 + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (!s.done(row0 + j) && x < __builtin_inff()) {
+      const float2 n = __builtin_bit_cast(float2, __hip_atomic_load(s.norm + row0 + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+      x += (value_of((uint32_t)(pair(i) >> 32)) - n.x) - n.y;
+    }
     key[i] = order_key(x);
   }
   for (int j = threadIdx.x; j < s.beams; j += SELECT_THREADS) len[j] = s.done(row0 + j) ? 1 : K;
@@ -266,9 +269,10 @@ __device__ __forceinline__ void select_row(const float* __restrict__ z, int64_t 
 #pragma unroll
     for (int w = 0; w < SELECT_THREADS / 64; ++w)
       if (ws[w] != 0.f) a += ws[w] * fast_exp2((finite_or_zero(wm[w]) - finite_or_zero(M)) * LOG2E);
-    const float lse = finite_or_zero(M) + logf(a);
-    if constexpr (BEAM) __hip_atomic_store(out.lse + out.row0 + row, lse, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    else out.lse[row] = lse;
+    const float2 norm{finite_or_zero(M), logf(a)};
+    if constexpr (BEAM)
+      __hip_atomic_store(out.norm + out.row0 + row, __builtin_bit_cast(unsigned long long, norm), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    else out.lse[row] = norm.x + norm.y;
   }
 
   auto group_keys = [&](auto f) {

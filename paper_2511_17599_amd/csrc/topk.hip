@@ -148,7 +148,7 @@ constexpr int REORDER_ROWS = 16;      // rows whose vectors a thread of the reor
 struct BeamPlan {
   TopkPlan t;
   int K;
-  int64_t off_cand, off_lse, off_arrived, bytes;
+  int64_t off_cand, off_norm, off_arrived, bytes;
 };
 bool make_beam_plan(int64_t batch, int64_t beams, int64_t d, int64_t V, int64_t n_out, flce_dtype dt, BeamPlan& b) {
   if (batch < 1 || beams < 1 || beams > BEAMS_MAX || n_out < 1 || n_out > BEAMS_MAX || batch > 0x7FFFFF00ll / beams || V < 1) return false;
@@ -157,7 +157,7 @@ bool make_beam_plan(int64_t batch, int64_t beams, int64_t d, int64_t V, int64_t 
   const int64_t rows = batch * beams;
   int64_t o = b.t.bytes;
   b.off_cand = o;    o = align_up(o + rows * b.K * 8, ALIGN);
-  b.off_lse = o;     o = align_up(o + rows * 4, ALIGN);
+  b.off_norm = o;    o = align_up(o + rows * 8, ALIGN);
   b.off_arrived = o; o = align_up(o + batch * 4, ALIGN);
   b.bytes = o;
   return true;
@@ -216,7 +216,7 @@ flce_status flce_beam_step(const void* H, const void* W, const float* scores, co
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   uint32_t* arrived = reinterpret_cast<uint32_t*>(ws + b.off_arrived);
   const flce::BeamStep out{scores, finished, 0, (int)beams, (int)n_out, eos_id, pad_id, scores_out, tokens_out, parents_out, finished_out,
-                           arrived, reinterpret_cast<unsigned long long*>(ws + b.off_cand), reinterpret_cast<float*>(ws + b.off_lse)};
+                           arrived, reinterpret_cast<unsigned long long*>(ws + b.off_cand), reinterpret_cast<unsigned long long*>(ws + b.off_norm)};
   return flce::run_topk(
       b.t, H, W, b.K, ws,
       [&](int64_t row0) {

@@ -9,6 +9,7 @@ pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
 import few_logits as F                                    # noqa: E402
+import test_gpu_beam as TB                                # noqa: E402
 import test_gpu_topk as TK                                # noqa: E402
 from conftest import set_plan                             # noqa: E402
 
@@ -66,3 +67,25 @@ def test_masks_beside_a_floor(K):
         wz, wids, wlse = F.topk(F.f64(full), K)
         assert np.array_equal(ids[rows].cpu().numpy(), wids) and np.array_equal(F.f64(z[rows]), wz)
         assert (np.abs(F.f64(lse[rows]) - wlse) <= F.lse_bound(wlse, V)).all()
+
+
+def log_softmax(z):
+    m = z.max(-1, keepdims=True)
+    return (z - m) - np.log(np.exp(z - m).sum(-1, keepdims=True))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("batch,beams,d,V,n_out", [(1, 4, 64, 301, 4), (3, 5, 72, 20011, 10), (30, 4, 64, 1501, 8)])
+def test_masks_in_a_beam_step(dtype, batch, beams, d, V, n_out):
+    """A beam whose logits are all the mask is uniform: its candidates are behind by log V, not level with its score."""
+    rng = np.random.default_rng(batch)
+    H, W = masked_operands(rng, batch * beams, d, V)
+    scores = np.float32(np.tile(-4 - 0.25 * np.arange(beams), (batch, 1)))
+    got = TB.step(H.reshape(batch, beams, d), W, scores, None, n_out, 2, 0, dtype)
+    logp = log_softmax(H @ W.T).reshape(batch, beams, V)
+    total = (scores.astype(np.float64)[..., None] + logp).reshape(batch, -1)
+    # equal logits of a beam are equal scores: by beam, then by token; scores of different logits are no nearer than a grid's step
+    order = np.argsort(-total, axis=1, kind="stable")[:, :n_out]
+    want = np.take_along_axis(total, order, 1)
+    assert np.array_equal(got[2], order // V) and np.array_equal(got[1], order % V)
+    assert (np.abs(got[0] - want) <= F.lse_bound(0.0, V) + 4 * F.U32 * (np.abs(want) + 40)).all()
