@@ -219,10 +219,10 @@ __global__ __launch_bounds__(L::THREADS, L::MIN_WAVES) void distill_tiles_kernel
         for (int r = 1; r < 16; ++r) bmax = fmaxf(bmax, z[r]);
         const float mn = fmaxf(m[j], bmax);
         const float ms = (mn == NEG_INF) ? 0.f : mn;     // nothing but padding so far: keep exp arguments finite
-        const float msl = -ms * a.z_scale;
+        // (the difference first: a logit's product with z_scale may be no number where the difference is one)
         float sum = 0.f;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sum += fast_exp2(fmaf(z[r], a.z_scale, msl));
+        for (int r = 0; r < 16; ++r) sum += fast_exp2((z[r] - ms) * a.z_scale);
         s[j] = s[j] * fast_exp2((m[j] - ms) * a.z_scale) + sum;
         m[j] = mn;
         __builtin_amdgcn_sched_barrier(0);     // one block at a time in VGPRs

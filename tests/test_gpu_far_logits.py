@@ -10,6 +10,7 @@ torch = pytest.importorskip("torch")
 
 import few_logits as F                                    # noqa: E402
 import test_gpu_beam as TB                                # noqa: E402
+import test_gpu_distill as TD                             # noqa: E402
 import test_gpu_topk as TK                                # noqa: E402
 from conftest import set_plan                             # noqa: E402
 
@@ -89,3 +90,55 @@ def test_masks_in_a_beam_step(dtype, batch, beams, d, V, n_out):
     want = np.take_along_axis(total, order, 1)
     assert np.array_equal(got[2], order // V) and np.array_equal(got[1], order % V)
     assert (np.abs(got[0] - want) <= F.lse_bound(0.0, V) + 4 * F.U32 * (np.abs(want) + 40)).all()
+
+
+def masked_student(rng, N, d, V, dtype):
+    """Operands, and the same without the mask's column: groups at the vocabulary's start, in its middle and at its end are masked in all
+    rows but row 0."""
+    H, W = TD.operands(rng, N, d, V, dtype)
+    H[:, 0], W[:, 0] = 0, 0
+    plain = H.copy(), W.copy()
+    H[1:, 0] = 1
+    free = np.arange(V // 3, V // 2)
+    W[:, 0] = LOW
+    W[free, 0] = 0
+    return H, W, free, plain
+
+
+@pytest.mark.parametrize("dtype,knobs", [("bf16", {}), ("f32", {}), ("bf16", dict(FLCE_GENERIC=1)), ("bf16", dict(FLCE_TILE=128)),
+                                         ("bf16", dict(FLCE_TILE=256))])
+@pytest.mark.parametrize("T", [1.0, 0.5, 3.0])
+@pytest.mark.parametrize("N,d,V", [(130, 72, 1601), (600, 96, 5003)])
+def test_masks_in_distillation(monkeypatch, dtype, knobs, T, N, d, V):
+    set_plan(monkeypatch, **knobs)
+    K = 20
+    rng = np.random.default_rng(N)
+    H, W, free, (H0, W0) = masked_student(rng, N, d, V, dtype)
+    ids = np.stack([rng.permutation(free)[:K] for _ in range(N)])
+    t = np.float32(rng.standard_normal((N, K)))
+    ids[::7, 3:] = -1
+    print(f"[case] masked distill {dtype} N={N} V={V} T={T} {knobs}", flush=True)
+    r = F.distill(H, W, ids, t.astype(np.float64), T, np.ones(N))
+    got = TD.call(F.on_gpu(H, dtype), F.on_gpu(W, dtype), torch.from_numpy(ids).cuda(), torch.from_numpy(t).cuda(), T, "sum")
+    # bounds: those of the same operands without the mask's column, whose products are exact (a probability of 0 where it masks)
+    assert (np.abs(F.f64(got["lse"]) - r["lse"]) <= F.logit_bound(H0, W0).max(1) / T + F.lse_bound(r["lse"], V)).all()
+    assert (np.abs(F.f64(got["rows"]) - r["rows"]) <= F.loss_bound(r, H0, W0, T)).all()
+    bH, bW = F.grad_bounds(r, H0, W0, T, dtype, False)    # (all columns but the mask's)
+    assert (np.abs(F.f64(got["dH"]) - r["dH"])[:, 1:] <= bH[:, 1:]).all()
+    assert (np.abs(F.f64(got["dW"]) - r["dW"])[:, 1:] <= bW[:, 1:]).all()
+
+
+def test_temperatures_that_take_logits_past_32_bits():
+    """Logits of 1e30 at a temperature of 1e-10: z / T is no number of 32 bits, the losses of rows with them are."""
+    N, d, V, K, T = 40, 64, 700, 5, 1e-10
+    H, W = np.zeros((N, d)), np.zeros((V, d))
+    H[:, 0], W[:, 0] = 1, -np.ldexp(1.0, 100)
+    W[100:110, 0] = 0
+    ids = np.tile(100 + np.arange(K), (N, 1))
+    t = np.zeros((N, K), np.float32)
+    got = TD.call(F.on_gpu(H, "f32"), F.on_gpu(W, "f32"), torch.from_numpy(ids).cuda(), torch.from_numpy(t).cuda(), T, "sum")
+    bound = F.lse_bound(np.log(10), V)
+    assert (np.abs(F.f64(got["lse"]) - np.log(10)) <= bound).all()
+    assert (np.abs(F.f64(got["rows"]) / T ** 2 - np.log(10 / K)) <= bound + (256 + 100) * F.U32 * (1 + np.log(K) + np.log(10))).all()
+    q = np.where(np.arange(V) < 100, 0, np.where(np.arange(V) < 100 + K, 0.1 - 1 / K, np.where(np.arange(V) < 110, 0.1, 0.0)))
+    assert (np.abs(F.f64(got["dW"])[:, 0] - T * N * q) <= T * N * (bound + 400 * F.U32)).all() and not got["dW"][:, 1:].any()
