@@ -67,6 +67,16 @@ def _workspace(N, d, V, dt, backward, device):
     return torch.empty(nb, dtype=torch.uint8, device=device), nb
 
 
+# The autograd nodes of the living losses that were made outside of a HIP graph's capture (see _refuse_capture).  One weak reference
+# per loss: what each call pays for it is a microsecond.
+_eager_nodes = set()
+
+
+def _remember(ctx):
+    if not torch.cuda.is_current_stream_capturing():
+        _eager_nodes.add(weakref.ref(ctx, _eager_nodes.discard))
+
+
 class _ScalarLoss(torch.autograd.Function):
     """Alg. 1 forward, Alg. 2 backward; mean or sum over the counted rows."""
 
@@ -83,6 +93,7 @@ class _ScalarLoss(torch.autograd.Function):
         _check(B.flce_forward(H2, W2, y, N, d, V, ignore_index, _RED[reduction], dt, loss, lse, ws, nb, st))
         ctx.save_for_backward(H2, W2, y, lse)
         ctx.meta = (H.shape, ignore_index, reduction)
+        _remember(ctx)
         return loss
 
     @staticmethod
@@ -124,6 +135,7 @@ class _RowLosses(torch.autograd.Function):
         _check(B.flce_forward_rows(H2, W2, y, N, d, V, ignore_index, label_smoothing, dt, rows, lse, ws, nb, st))
         ctx.save_for_backward(H2, W2, y, lse)
         ctx.meta = (H.shape, ignore_index, label_smoothing)
+        _remember(ctx)
         return rows if targets.dim() == 1 else rows.reshape(targets.shape)
 
     @staticmethod
@@ -143,33 +155,6 @@ class _RowLosses(torch.autograd.Function):
         return dH if dH.shape == shape else dH.reshape(shape), dW, None, None, None
 
 
-_eager_graphs = {}
-
-
-class _EagerGraph:
-    """Lives as long as the autograd graph of an eager loss does; its leaves are known that long."""
-    __slots__ = ("key",)
-
-    def __init__(self, leaves):
-        self.key = id(self)
-        _eager_graphs[self.key] = [weakref.ref(t) for t in leaves]
-
-    def __del__(self, graphs=_eager_graphs):
-        graphs.pop(self.key, None)
-
-
-def _leaves(H, W):
-    return [t for t in (H, W) if t.requires_grad and t.is_leaf] if torch.is_grad_enabled() else []
-
-
-def _known(loss, H, W):
-    """`loss` with its leaves known as long as its graph lives (see _graph_of)."""
-    leaves = _leaves(H, W)
-    if leaves and loss.is_cuda and not torch.cuda.is_current_stream_capturing():
-        loss.grad_fn.graph = _EagerGraph(leaves)
-    return loss
-
-
 def linear_cross_entropy(H, W, targets, ignore_index=-100, reduction="mean", label_smoothing=0.0):
     """Cross-entropy of softmax(H . W^T) against `targets` without the logits tensor.
 
@@ -182,8 +167,8 @@ def linear_cross_entropy(H, W, targets, ignore_index=-100, reduction="mean", lab
     if reduction != "none":
         if label_smoothing != 0.0:
             raise ValueError("label smoothing is available with reduction='none' only")
-        return _known(_ScalarLoss.apply(H, W, targets, int(ignore_index), reduction), H, W)
-    return _known(_RowLosses.apply(H, W, targets, int(ignore_index), float(label_smoothing)), H, W)
+        return _ScalarLoss.apply(H, W, targets, int(ignore_index), reduction)
+    return _RowLosses.apply(H, W, targets, int(ignore_index), float(label_smoothing))
 
 
 def _launch(call, device, *args):
@@ -243,25 +228,23 @@ def linear_topk(H, W, k):
     return logits.reshape(*lead, k), ids.reshape(*lead, k), lse.reshape(lead)
 
 
-def _graph_of(H, W):
+def _refuse_capture(H, W):
     """While an autograd graph made outside a HIP graph's capture lives, torch's gradient accumulators of its leaves belong to the
     stream it was made on; a backward captured for the same leaves would wait for that stream, which ends the process.  Such a
     capture is refused."""
-    leaves = _leaves(H, W)
-    if not leaves:
-        return None
-    if H.is_cuda and torch.cuda.is_current_stream_capturing():
-        if any(r() is t for refs in list(_eager_graphs.values()) for r in refs for t in leaves):
-            raise RuntimeError("an eager loss of the same H or W is alive: drop it before capturing a distillation")
-        return None
-    return _EagerGraph(leaves)
+    if not (H.is_cuda and torch.is_grad_enabled() and torch.cuda.is_current_stream_capturing()):
+        return
+    mine = {torch.autograd.graph.get_gradient_edge(t).node for t in (H, W) if t.requires_grad and t.is_leaf}
+    living = [node for node in (ref() for ref in _eager_nodes.copy()) if node is not None]
+    if any(edge in mine for node in living for edge, _ in node.next_functions):
+        raise RuntimeError("an eager loss of the same H or W is alive: drop it before capturing a distillation")
 
 
 class _Distillation(torch.autograd.Function):
     """Loss over a teacher's lists; mean or sum over the rows that count, or one loss per row."""
 
     @staticmethod
-    def forward(ctx, H, W, ids, logits, temperature, reduction, graph):
+    def forward(ctx, H, W, ids, logits, temperature, reduction):
         H2, W2 = _operands(H, W)
         (N, d), V, dt, dev = H2.shape, W2.shape[0], _DT[H2.dtype], H2.device
         K = ids.shape[-1]
@@ -278,7 +261,7 @@ class _Distillation(torch.autograd.Function):
                 None if rows else out, out if rows else None, saved + ns, saved, ws, nb)
         ctx.save_for_backward(H2, W2, ids2, keep)
         ctx.meta = (H.shape, temperature, reduction, K, ns)
-        ctx.graph = graph
+        _remember(ctx)
         return out
 
     @staticmethod
@@ -301,7 +284,7 @@ class _Distillation(torch.autograd.Function):
         saved = keep.data_ptr()
         _launch(B.flce_distill_backward, dev, H2, W2, ids2, saved + ns, saved, N, d, V, K, temperature,
                 _RED.get(reduction, B.FLCE_REDUCE_SUM), dt, None if rows else g, g if rows else None, dH, dW, ws, nb)
-        return dH if dH.shape == shape else dH.reshape(shape), dW, None, None, None, None, None
+        return dH if dH.shape == shape else dH.reshape(shape), dW, None, None, None, None
 
 
 def linear_distillation(H, W, teacher_ids, teacher_logits, temperature=1.0, reduction="mean"):
@@ -320,7 +303,8 @@ def linear_distillation(H, W, teacher_ids, teacher_logits, temperature=1.0, redu
         raise TypeError("teacher_ids are integers, teacher_logits are floating point")
     if teacher_ids.shape != teacher_logits.shape or teacher_ids.dim() != H.dim() or teacher_ids.shape[:-1] != H.shape[:-1]:
         raise ValueError("shapes: H [..., d], teacher_ids and teacher_logits [..., K]")
-    return _Distillation.apply(H, W, teacher_ids, teacher_logits, float(temperature), reduction, _graph_of(H, W))
+    _refuse_capture(H, W)
+    return _Distillation.apply(H, W, teacher_ids, teacher_logits, float(temperature), reduction)
 
 
 def beam_step(H, W, scores, finished=None, n_out=None, eos_id=-1, pad_id=0):
