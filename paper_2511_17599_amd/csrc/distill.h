@@ -384,13 +384,14 @@ __global__ __launch_bounds__(64 * R) void distill_rows_kernel(DistillRowArgs a) 
       const float mw[2] = {m, __shfl_xor(m, o, 64)}, aw[2] = {sum, __shfl_xor(sum, o, 64)};
       merge_scaled<2>(mw, aw, a.z_scale, m, sum);
     }
-    const float lse = fmaf(m, a.inv_T, logf(sum));
+    // (m / T and log sum are kept apart in the loss: where the largest logit is far from 0 their sum has lost the logarithm)
+    const float log_a = logf(sum), lse = fmaf(m, a.inv_T, log_a);
     counts = list.counts;
     oor = list.out_of_range;
     float kl = 0.f;
 #pragma unroll
     for (int u = 0; u < RowList::U; ++u)
-      if (list.id[u] >= 0 && list.p[u] != 0.f) kl += list.p[u] * ((list.x[u] - list.log_sum) + fmaf(-z[u], a.inv_T, lse));
+      if (list.id[u] >= 0 && list.p[u] != 0.f) kl += list.p[u] * ((list.x[u] - list.log_sum) + fmaf(m - z[u], a.inv_T, log_a));
     kl = wave_sum(kl);
     loss = counts ? a.temperature * a.temperature * kl : 0.f;
     // every entry against all of the row's, eight at a time (a wavefront reads what it wrote: LDS operations of one are in order)

@@ -142,3 +142,19 @@ def test_temperatures_that_take_logits_past_32_bits():
     assert (np.abs(F.f64(got["rows"]) / T ** 2 - np.log(10 / K)) <= bound + (256 + 100) * F.U32 * (1 + np.log(K) + np.log(10))).all()
     q = np.where(np.arange(V) < 100, 0, np.where(np.arange(V) < 100 + K, 0.1 - 1 / K, np.where(np.arange(V) < 110, 0.1, 0.0)))
     assert (np.abs(F.f64(got["dW"])[:, 0] - T * N * q) <= T * N * (bound + 400 * F.U32)).all() and not got["dW"][:, 1:].any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_losses_of_rows_that_are_all_mask(dtype):
+    """Such a row is uniform: its loss is log V minus the entropy of its list."""
+    N, d, V, K = 90, 64, 1501, 9
+    rng = np.random.default_rng(8)
+    H, W = TD.operands(rng, N, d, V, dtype)
+    H[:, 0], W[:, 0] = 0, LOW
+    H[5:9, 0] = 1
+    ids = np.stack([rng.permutation(V)[:K] for _ in range(N)])
+    t = np.float32(rng.standard_normal((N, K)))
+    got = TD.call(F.on_gpu(H, dtype), F.on_gpu(W, dtype), torch.from_numpy(ids).cuda(), torch.from_numpy(t).cuda(), 1.0, "sum")
+    p = F.shares(ids, t.astype(np.float64), 1.0, V)[0]
+    want = (p * (np.log(p) + np.log(V))).sum(1)
+    assert (np.abs(F.f64(got["rows"]) - want)[5:9] <= F.lse_bound(0.0, V) + (256 + 100) * F.U32 * (1 + np.log(V) + 8)).all()
