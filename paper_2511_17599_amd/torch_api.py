@@ -228,16 +228,27 @@ def linear_topk(H, W, k):
     return logits.reshape(*lead, k), ids.reshape(*lead, k), lse.reshape(lead)
 
 
+def _accumulators(nodes):
+    """The gradient accumulators that the autograd graphs behind `nodes` end in."""
+    seen, todo = set(), list(nodes)
+    while todo:
+        node = todo.pop()
+        if node not in seen:
+            seen.add(node)
+            todo += [n for n, _ in node.next_functions if n is not None]
+    return {node for node in seen if not node.next_functions}
+
+
 def _refuse_capture(H, W):
-    """While an autograd graph made outside a HIP graph's capture lives, torch's gradient accumulators of its leaves belong to the
-    stream it was made on; a backward captured for the same leaves would wait for that stream, which ends the process.  Such a
-    capture is refused."""
+    """While an autograd graph made outside a HIP graph's capture lives, torch's gradient accumulators of its leaves (H, W or what they
+    were computed from) belong to the stream it was made on; a backward captured for the same leaves would wait for that stream,
+    which ends the process.  Such a capture is refused."""
     if not (H.is_cuda and torch.is_grad_enabled() and torch.cuda.is_current_stream_capturing()):
         return
-    mine = {torch.autograd.graph.get_gradient_edge(t).node for t in (H, W) if t.requires_grad and t.is_leaf}
+    mine = [torch.autograd.graph.get_gradient_edge(t).node for t in (H, W) if t.requires_grad]
     living = [node for node in (ref() for ref in _eager_nodes.copy()) if node is not None]
-    if any(edge in mine for node in living for edge, _ in node.next_functions):
-        raise RuntimeError("an eager loss of the same H or W is alive: drop it before capturing a distillation")
+    if mine and not _accumulators(mine).isdisjoint(_accumulators(living)):
+        raise RuntimeError("an eager loss of the same leaves is alive: drop it before capturing a distillation")
 
 
 class _Distillation(torch.autograd.Function):
@@ -295,7 +306,8 @@ def linear_distillation(H, W, teacher_ids, teacher_logits, temperature=1.0, redu
     the vocabulary's logits / T, T = temperature.  reduction: "mean" (over the rows that have an entry), "sum" or "none".
     Rows without an entry, and rows with an id beyond the vocabulary, have loss and gradient 0.
 
-    Forward and backward can be captured into a HIP graph while no autograd graph made outside of it holds H or W as a leaf.
+    Forward and backward can be captured into a HIP graph while no autograd graph made outside of it has a leaf in common with them (H, W or
+    the parameters they come from).  Beside a living eager loss of this module the call is refused, under torch.no_grad() it is not.
     """
     if reduction not in ("mean", "sum", "none"):
         raise ValueError("reduction must be 'mean', 'sum' or 'none'")

@@ -83,3 +83,16 @@ def test_a_loss_costs_little_to_remember(capturing, monkeypatch):
     cost = min(times[False]) - min(times[True])
     print(f"{cost * 1e6:.2f} us of {min(times[False]) * 1e6:.1f}")
     assert cost < 3e-6
+
+
+def test_accumulators_behind_the_states(capturing):
+    """In a model the leaves are the parameters that the states were computed from."""
+    H, W, y, _ = case()
+    P, x = torch.randn(8, 8, requires_grad=True), torch.randn(4, 8)
+    loss = A.linear_cross_entropy(torch.tanh(x @ P), W, y)
+    node = [r() for r in A._eager_nodes if r() is loss.grad_fn]
+    at = [torch.autograd.graph.get_gradient_edge(t).node for t in (P, W)]
+    assert len(node) == 1 and A._accumulators(node) == set(at)
+    other = torch.relu(x @ P)
+    assert A._accumulators([torch.autograd.graph.get_gradient_edge(other).node]) == {at[0]}
+    assert A._accumulators([torch.autograd.graph.get_gradient_edge(H).node]).isdisjoint(at)
