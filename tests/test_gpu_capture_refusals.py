@@ -29,3 +29,19 @@ def test_distillation_beside_a_living_loss_of_the_same_parameters(monkeypatch, e
     del loss
     linear_distillation(torch.relu(x @ P), W, *lists).backward()
     assert P.grad is not None and W.grad is not None
+
+
+@pytest.mark.parametrize("reduction", ["mean", "none"])
+@pytest.mark.parametrize("eager", ["distillation", "cross_entropy"])
+def test_cross_entropy_beside_a_living_loss_of_the_same_parameters(monkeypatch, eager, reduction):
+    x, P, W, lists, y = case()
+    H = torch.tanh(x @ P)
+    loss = linear_distillation(H, W, *lists) if eager == "distillation" else linear_cross_entropy(H, W, y, reduction=reduction)
+    del H
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    again = linear_cross_entropy(x @ P, W, y, reduction=reduction).sum()
+    with pytest.raises(RuntimeError, match="alive"):
+        again.backward()
+    del loss, again
+    linear_cross_entropy(x @ P, W, y, reduction=reduction).sum().backward()
+    assert P.grad is not None and W.grad is not None
