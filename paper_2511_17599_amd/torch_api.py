@@ -269,6 +269,18 @@ def _refuse_capture(H, W):
             raise RuntimeError("an eager loss of the same leaves is alive: drop it before capturing a distillation")
 
 
+class _Once(torch.autograd.Function):
+    """Gradients that the library has filled have no graph of their own: where torch is to keep one (create_graph), it ends here."""
+
+    @staticmethod
+    def forward(ctx, dH, dW, H, W, grad):
+        return dH, dW
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("the gradients of linear_distillation cannot be differentiated")
+
+
 class _Distillation(torch.autograd.Function):
     """Loss over a teacher's lists; mean or sum over the rows that count, or one loss per row."""
 
@@ -288,8 +300,8 @@ class _Distillation(torch.autograd.Function):
         saved = keep.data_ptr()
         _launch(B.flce_distill_forward, dev, H2, W2, ids2, t2, N, d, V, K, temperature, _RED.get(reduction, B.FLCE_REDUCE_SUM), dt,
                 None if rows else out, out if rows else None, saved + ns, saved, ws, nb)
-        ctx.save_for_backward(H2, W2, ids2, keep)
-        ctx.meta = (H.shape, temperature, reduction, K, ns)
+        ctx.save_for_backward(H, W, ids2, keep)
+        ctx.meta = (temperature, reduction, K, ns)
         _remember(ctx, _stream(dev))
         return out
 
@@ -297,9 +309,9 @@ class _Distillation(torch.autograd.Function):
     def backward(ctx, grad):
         if ctx.stream is None:
             _refuse_captured_backward(ctx)
-        H2, W2, ids2, keep = ctx.saved_tensors
-        shape, temperature, reduction, K, ns = ctx.meta
-        (N, d), V, dt, dev = H2.shape, W2.shape[0], _DT[H2.dtype], H2.device
+        H, W, ids2, keep = ctx.saved_tensors
+        temperature, reduction, K, ns = ctx.meta
+        N, (V, d), dt, dev = ids2.numel() // K, W.shape, _DT[H.dtype], H.device
         # The kernels read the gradient where it is; one that is only marked as negated or zero is made first.
         g = grad
         if g.dtype is not torch.float32 or g.device != dev:
@@ -309,13 +321,15 @@ class _Distillation(torch.autograd.Function):
         rows = reduction == "none"
         if rows:
             g = g.contiguous()
-        dH = torch.empty_like(H2)
-        dW = torch.empty_like(W2)
+        dH = torch.empty_like(H)
+        dW = torch.empty_like(W)
         ws, nb = _scratch(B.flce_distill_workspace_bytes(N, d, V, K, dt, 1), dev, "as in the forward")
         saved = keep.data_ptr()
-        _launch(B.flce_distill_backward, dev, H2, W2, ids2, saved + ns, saved, N, d, V, K, temperature,
+        _launch(B.flce_distill_backward, dev, H, W, ids2, saved + ns, saved, N, d, V, K, temperature,
                 _RED.get(reduction, B.FLCE_REDUCE_SUM), dt, None if rows else g, g if rows else None, dH, dW, ws, nb)
-        return dH if dH.shape == shape else dH.reshape(shape), dW, None, None, None, None
+        if torch.is_grad_enabled():
+            dH, dW = _Once.apply(dH, dW, H, W, grad)
+        return dH, dW, None, None, None, None
 
 
 def linear_distillation(H, W, teacher_ids, teacher_logits, temperature=1.0, reduction="mean"):
@@ -324,7 +338,8 @@ def linear_distillation(H, W, teacher_ids, teacher_logits, temperature=1.0, redu
     teacher_ids [..., K] (int64, negative: no entry) and teacher_logits [..., K] (float, no gradient) with the leading shape
     of H, K <= 256, as linear_topk gives them.  Per row T^2 KL(p || q) with p = softmax over the list's logits / T and q = softmax over
     the vocabulary's logits / T, T = temperature.  reduction: "mean" (over the rows that have an entry), "sum" or "none".
-    Rows without an entry, and rows with an id beyond the vocabulary, have loss and gradient 0.
+    Rows without an entry, and rows with an id beyond the vocabulary, have loss and gradient 0.  The gradients cannot be differentiated
+    again: that raises.
 
     Forward and backward can be captured into a HIP graph while no autograd graph made outside of it has a leaf in common with them (H, W or
     the parameters they come from).  Beside a living eager loss of this module the call is refused, under torch.no_grad() it is not.
@@ -336,7 +351,8 @@ def linear_distillation(H, W, teacher_ids, teacher_logits, temperature=1.0, redu
     if teacher_ids.shape != teacher_logits.shape or teacher_ids.dim() != H.dim() or teacher_ids.shape[:-1] != H.shape[:-1]:
         raise ValueError("shapes: H [..., d], teacher_ids and teacher_logits [..., K]")
     _refuse_capture(H, W)
-    return _Distillation.apply(H, W, teacher_ids, teacher_logits, float(temperature), reduction)
+    # (copies are made here, in the autograd graph, so that H and W are what the backward keeps)
+    return _Distillation.apply(H.contiguous(), W.contiguous(), teacher_ids, teacher_logits, float(temperature), reduction)
 
 
 def beam_step(H, W, scores, finished=None, n_out=None, eos_id=-1, pad_id=0):

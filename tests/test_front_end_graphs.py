@@ -127,3 +127,28 @@ def test_captures_beside_losses_of_a_side_stream(capturing, monkeypatch):
     capturing[0] = True
     A.linear_cross_entropy(H, W, y).backward()
     assert living.requires_grad
+
+
+@pytest.mark.parametrize("lead", [(4,), (2, 2)])
+@pytest.mark.parametrize("strided", [False, True])
+def test_distillation_is_differentiated_once(capturing, monkeypatch, lead, strided):
+    """The library's gradients have no graph of their own: a penalty on what follows from them raises where it would lose the loss's part,
+    however it is differentiated."""
+    _, W, _, lists = case()
+    lists = tuple(t.reshape(*lead, 2) for t in lists)
+    W.requires_grad_(False)
+    monkeypatch.setattr(A, "_launch", lambda call, device, *args: [t.fill_(1) for t in args if torch.is_tensor(t) and t.shape == W.shape])
+    P, x = torch.randn(8, 8, requires_grad=True), torch.randn(*lead, 8)
+
+    def states():
+        h = torch.tanh(x @ P)
+        return torch.stack([h, h], -1)[..., 0] if strided else h
+
+    for take in (lambda g: torch.autograd.grad((g * g).sum(), P), lambda g: (g * g).sum().backward()):
+        loss = A.linear_distillation(states(), W, *lists)
+        g, = torch.autograd.grad(loss, P, create_graph=True)
+        assert g.requires_grad
+        with pytest.raises(RuntimeError, match="cannot be differentiated"):
+            take(g)
+    A.linear_distillation(states(), W, *lists).backward()
+    assert P.grad is not None and not P.grad.requires_grad
