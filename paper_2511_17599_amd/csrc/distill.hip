@@ -45,7 +45,7 @@ namespace {
 
 struct DistillPlan {
   Plan p;
-  int tile, n_blk, n_win;
+  int n_blk, n_win;
   int64_t off_blk_loss, off_blk_cnt, off_blk_oor, off_part, off_begin, off_entries, off_HT, fwd_bytes;
 };
 
@@ -53,21 +53,26 @@ bool make_distill_plan(int parts, int64_t N, int64_t d, int64_t V, int64_t K, fl
   if (!make_plan(parts, N, d, V, dt, x.p) || K < 1 || K > DISTILL_MAX) return false;
   const Plan& p = x.p;
   if (parts & PLAN_FORWARD) {
-    x.tile = p.esize == 2 && !p.fast ? TILE : p.fwd_tile;
+    int64_t tile = 0, buckets = 0;          // of the loop: edge, and wavefronts that the lists of a tile are sorted for
+    with_forward_loop(p, [&](auto tag) -> flce_status {
+      using L = typename decltype(tag)::L;
+      tile = L::TILE;
+      buckets = 2 * list_waves<L>();
+      return FLCE_OK;
+    });
     x.n_blk = (int)ceil_div(N, distill_rows_per_block(N));
     // The cross-entropy's windows, but in fp32 where they leave CUs idle as many as give every CU two workgroups, down to a tile each
     // (its 64-row tiles are planned by 256 positions: 256 x 256 x 4096, 256 tiles, 37 us as four each of 64 workgroups, 11 as one each).
-    const int64_t rt = ceil_div(N, x.tile), vt = ceil_div(V, x.tile);
+    const int64_t n_rt = ceil_div(N, tile), n_vt = ceil_div(V, tile);
     x.n_win = p.n_win;
-    if (p.esize == 4 && rt * x.n_win < 2 * NUM_CU) x.n_win = (int)std::min(vt, std::max<int64_t>(x.n_win, ceil_div(2 * NUM_CU, rt)));
-    const int64_t n_rt = ceil_div(N, x.tile), n_vt = ceil_div(V, x.tile);
+    if (p.esize == 4 && n_rt * x.n_win < 2 * NUM_CU) x.n_win = (int)std::min(n_vt, std::max<int64_t>(x.n_win, ceil_div(2 * NUM_CU, n_rt)));
     int64_t o = ALIGN;
     x.off_blk_loss = o; o = align_up(o + (int64_t)x.n_blk * 4, ALIGN);
     x.off_blk_cnt = o;  o = align_up(o + (int64_t)x.n_blk * 4, ALIGN);
     x.off_blk_oor = o;  o = align_up(o + (int64_t)x.n_blk * 4, ALIGN);
     x.off_part = o;     o = align_up(o + 2ll * x.n_win * p.npad * 4, ALIGN);
-    x.off_begin = o;    o = align_up(o + n_rt * (n_vt * (x.tile == TILE && !p.fast ? 8 : 4) + 1) * 4, ALIGN);
-    x.off_entries = o;  o = align_up(o + n_rt * x.tile * K * 4, ALIGN);
+    x.off_begin = o;    o = align_up(o + n_rt * (n_vt * buckets + 1) * 4, ALIGN);
+    x.off_entries = o;  o = align_up(o + n_rt * tile * K * 4, ALIGN);
     x.off_HT = o;       if (p.fwd_copy) o = align_up(o + packed_block_offset(p.n_rb, (int)d), ALIGN);
     x.fwd_bytes = o;
   }
@@ -143,8 +148,8 @@ flce_status flce_distill_forward(const void* H, const void* W, const int64_t* te
     const int n_rb = (int)ceil_div(N, L::TILE), n_vt = (int)ceil_div(V, L::TILE), items = n_rb * x.n_win;
     {
       ProfScope ps(FLCE_PROF_FWD_EPILOGUE, st);
-      distill_lists_kernel<L::TILE, L::THREADS / 128><<<(unsigned)n_rb, 1024, 0, st>>>(teacher_ids, teacher_logits, (int)N, (int)V, (int)K, n_vt, begin, entries,
-                                                                     saved, hdr);
+      distill_lists_kernel<L::TILE, list_waves<L>()><<<(unsigned)n_rb, 1024, 0, st>>>(teacher_ids, teacher_logits, (int)N, (int)V, (int)K, n_vt,
+                                                                                      begin, entries, hdr);
     }
     {
       // one workgroup per (row block, window), with the tuned loop a round of them per launch, as the cross-entropy's forward
