@@ -70,6 +70,32 @@ def test_masks_beside_a_floor(K):
         assert (np.abs(F.f64(lse[rows]) - wlse) <= F.lse_bound(wlse, V)).all()
 
 
+@pytest.mark.parametrize("K", [5, 60])
+def test_infinities_and_nan_beside_a_floor(K):
+    """Every place of the lists of rows with infinities in the first part, with and without NaN behind it, and of rows of nothing but NaN."""
+    N, d, V = 2100, 1024, 50000
+    H, W = F.grid_operands(np.random.default_rng(V + K), N, d, V)
+    H[:, 1:4], W[:, 1:4] = 0, 0
+    Hg, Wg = F.on_gpu(H, "bf16"), F.on_gpu(W, "bf16")
+    Wg[100:100 + 64 * (K + 3):64, 2] = HIGH               # rows 2 .. 5: more infinities than places (a product past 32 bits)
+    Wg[V - 9, 2] = LOW
+    Hg[2:6, 2] = 4
+    Hg[10:12, 2] = -4                                     # rows 10, 11: -inf there, one infinity at the end
+    Wg[:, 3] = 1
+    Wg[V - 9, 3] = 0
+    Hg[6:10, 3] = float("inf")                            # rows 6 .. 9: infinities everywhere, NaN at one place of the end
+    Hg[12] = float("nan")
+    Hg[13, 5] = float("inf")                              # both infinities, and NaN where W is 0
+    z, ids, lse = TK.call(Hg, Wg, K)
+    full = Hg[:16].float() @ Wg.float().t()
+    wz, wids, wlse = F.topk(F.f64(full), K)
+    assert np.isinf(wz[2:6]).all() and np.isnan(wz[6:10, 0]).all() and np.isnan(wz[12]).all()
+    assert np.array_equal(ids[:16].cpu().numpy(), wids) and np.array_equal(F.f64(z[:16]), wz, equal_nan=True)
+    got, fin = F.f64(lse[:16]), np.isfinite(wlse)
+    assert np.array_equal(got[~fin], wlse[~fin], equal_nan=True)
+    assert (np.abs(got[fin] - wlse[fin]) <= F.lse_bound(wlse[fin], V)).all()
+
+
 def log_softmax(z):
     m = z.max(-1, keepdims=True)
     return (z - m) - np.log(np.exp(z - m).sum(-1, keepdims=True))
