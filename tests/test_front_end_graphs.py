@@ -14,7 +14,7 @@ from paper_2511_17599_amd import torch_api as A
 def capturing(monkeypatch):
     """The front end on CPU tensors; the returned list says whether a capture is to be seen."""
     state = [False]
-    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: state[0])
+    monkeypatch.setattr(A, "_capturing", lambda tensor: state[0])
     monkeypatch.setattr(A, "_stream", lambda device: 0)
     monkeypatch.setattr(A, "_prepare", lambda H, W, y: (H.reshape(-1, H.shape[-1]), W, y.reshape(-1)))
     monkeypatch.setattr(A, "_operands", lambda H, W: (H.reshape(-1, H.shape[-1]), W))
@@ -81,7 +81,7 @@ def test_a_loss_costs_little_to_remember(capturing, monkeypatch):
         return count[0]
 
     here = calls()
-    monkeypatch.setattr(A, "_remember", lambda ctx, stream: None)
+    monkeypatch.setattr(A, "_remember", lambda *args: None)
     without = calls()
     print(here, without)
     assert here - without <= 5

@@ -1,4 +1,4 @@
-"""GPU: which captures the front end refuses.  (The checks alone: nothing is captured here.)"""
+"""GPU: which captures the front end refuses (the checks alone, nothing is captured there), and that others go through."""
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -45,3 +45,27 @@ def test_cross_entropy_beside_a_living_loss_of_the_same_parameters(monkeypatch, 
     del loss, again
     linear_cross_entropy(x @ P, W, y, reduction=reduction).sum().backward()
     assert P.grad is not None and W.grad is not None
+
+
+@pytest.mark.parametrize("reduction", ["mean", "none"])
+def test_a_captured_cross_entropy_step(reduction):
+    _, P, W, _, y = case()
+    up = None if reduction == "mean" else torch.linspace(0.5, 1, 8, device="cuda")
+    H = torch.randn(8, 16, device="cuda", requires_grad=True)
+
+    def step():
+        loss = linear_cross_entropy(H, W, y, reduction=reduction)
+        return (loss.detach(), *torch.autograd.grad(loss, (H, W), up))
+
+    want = [t.clone() for t in step()]                             # (no eager graph lives behind it)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = step()
+    for rep in range(3):
+        for t in got:
+            t.fill_(7)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), rep
