@@ -349,7 +349,9 @@ flce_status flce_topk(const void* H, const void* W, int64_t N, int64_t d, int64_
  *                   backward takes lse and saved back, with the same ids, K and T.
  *   grad_loss     : device, 1 float, the upstream gradient of the scalar loss, or NULL;
  *   grad_rows     : device, N floats, of the losses per row (sum semantics), or NULL: exactly one of the two.
- * G = dloss/dZ is rounded to `dt` before the two contractions, as flce_backward's and flce_backward_rows' is.
+ * G = dloss/dZ is rounded to `dt` before the two contractions, as flce_backward's and flce_backward_rows' is.  Its probabilities come from
+ * lse and are off by |lse| 2^-24 beside the logits' own rounding; where |lse| log2(e) is past the range of 32 bits (a row whose logits are all
+ * near the lowest number) there are none and the gradients are not finite.  Losses have no such limit: they take (Z_iv - max Z_i) / T.
  * Workspaces: flce_distill_workspace_bytes(N, d, V, K, dt, for_backward) bytes, 0 for an invalid shape.  Forward: 8 bytes per window
  * and row, the lists by tile (4 bytes per entry, and per pair of a row and a vocabulary tile), flce_forward's copy of H; backward:
  * flce_backward's.
@@ -392,7 +394,7 @@ flce_status flce_beam_step(const void* H, const void* W, const float* scores, co
  * (layers, keys and values), b < batch, j < beams_out.  Rows of one o lie row_stride bytes apart ([batch][beams]), the o outer_stride
  * bytes (any strides and alignment; multiples of 16 bytes are fast).  What lies between row_bytes and row_stride is left as it
  * was.  src and dst may be the same memory with the same strides, for beams_in == beams_out <= 16 (rows that keep their place
- * are not touched); otherwise they must not overlap.
+ * are not touched); otherwise the ranges from their first to their last byte must not overlap (rows of one between those of the other do).
  *   beams_in, beams_out : 1 .. 64.    parents : device, batch*beams_out int64.
  *   status_out : device, one int32, or NULL: set to FLCE_ERR_TARGET_RANGE where a parent is outside [0, beams_in) (its row is left
  *                as it was), never cleared.

@@ -40,8 +40,8 @@ __device__ __forceinline__ void for_each_value(const float* p, F f) {
 // One workgroup: 16 MB vocabulary rows by 16 NT token rows.  Its four wavefronts take U consecutive K steps (64 U bytes of a row of W) in
 // turn, and their sums are added in wavefront order through LDS.
 // W goes from memory to the matrix instruction's registers without a stop in LDS: no element of it is used twice by a wavefront.
-// Bound by the read of W (128256 x 4096 in bf16: 1 row 200 us or 5.2 TB/s, 32 rows 227); H (N d elements, from the L2) is read once per
-// workgroup.  Tried and no faster: a wavefront per group with H shared through LDS or the L1 (32 rows 251 to
+// Bound by the read of W (128256 x 4096 in bf16: this kernel alone with 1 row 195 us or 5.4 TB/s, with 32 rows 227); H (N d elements, from the
+// L2) is read once per workgroup.  Tried and no faster: a wavefront per group with H shared through LDS or the L1 (32 rows 251 to
 // 283), the next run's loads issued ahead of the products (registers for them cost more wavefronts than they gain), loads of W
 // that pass the caches (291).
 template <typename T, int MB, int NT, int U>
@@ -145,13 +145,16 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void few_rows_kernel(const T* __res
 
 // Consecutive positions per group (16, 32 or 64): as many as leave 512 workgroups, two per CU.
 inline int few_rows_group(int64_t V) { return V >= 64 * 512 ? 64 : V >= 32 * 512 ? 32 : 16; }
-// Whether this kernel takes a call (otherwise the tiles of the forward's loop do).  Both, us, selection included: bf16 128256 x 4096
-// 4 rows 208 / 237, 32 rows 233 / 243, 64 rows 288 / 251; 32000 x 1024 32 rows 26.9 / 27.0, 64 rows 36.7 / 27.3; 8192 x 4096 64 rows
-// 46.7 / 53.7; fp32 50257 x 768 4 rows 43 / 86, 32 rows 61 / 87, 64 rows 91 / 87.
+// Whether this kernel takes a call (otherwise the tiles of the forward's loop do, whose logits take 256 rows of the workspace however few are
+// asked for: 131 MB at 128256 positions, this kernel's one row 0.5).  Whole calls of the selection, this kernel / tiles, us: bf16 50257 x 768
+// 1 row 27.6 / 31.0, 4 rows 25.5 / 28.6, 32 rows 33.2 / 30.9; 16000 x 1024 1 row 13.6 / 16.4, 32 rows 20.5 / 17.2, 64 rows 28.4 / 18.1; 8192 x 4096
+// 64 rows 46.8 / 52.4; 32000 x 1024 32 rows 26.4 / 24.2, 64 rows 36.3 / 25.2; 128256 x 4096 1 row 203 / 192, 32 rows 236 / 208, 64 rows 277 / 226;
+// fp32 50257 x 768 4 rows 42 / 82, 32 rows 60 / 84, 64 rows 90 / 83; 128256 x 4096 1 row 391 / 724, 32 rows 508 / 776.
 inline bool few_rows_ok(int64_t N, int64_t V) { return N <= 32 || (N <= 64 && few_rows_group(V) == 16); }
 
-// 17 to 32 rows over a long vocabulary take two groups per workgroup and longer runs (32 rows of 128256 x 4096: 247 us, one group 264); elsewhere
-// the registers that takes cost more than it gives (1 row 217, two groups 221).
+// 17 to 32 rows over a long vocabulary take two groups per workgroup and longer runs, which pays with whole rounds of workgroups (whole calls:
+// 32 rows of 128256 x 4096 236 us, one group 253; fp32 508, one group 523) and loses just past one (516 workgroups: 32 rows of 66000 x 4096 189,
+// one group 154).  Up to 16 rows the registers that it takes cost more than it gives (1 row 203, two groups 234).
 template <typename T>
 void launch_few_rows(const T* H, const T* W, int N, int d, int V, float* z, int64_t ldz, float2* stats, int64_t ld_stats, ZeroWords zero,
                      hipStream_t st) {
